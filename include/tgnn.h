@@ -361,6 +361,43 @@ int32_t tgnn_profile_enable(tgnn_ctx* ctx, uint32_t stage_mask);
 int32_t tgnn_profile_every(tgnn_ctx* ctx, int32_t n);
 int32_t tgnn_profile_read(tgnn_ctx* ctx, int32_t stage, int32_t* out_count, double* out_total_ms);
 
+/* ---- Operators on sequences of events and what a layer of them takes to train.
+ * They need no context: a call works on what it is given, on `stream`, launches kernels and nothing else, and can be
+ * captured into a graph.  Where one needs scratch memory the caller hands it over (workspace, 16-byte aligned,
+ * tgnn_..._workspace_bytes; what it holds before and after does not matter; two calls that may overlap in time need two).
+ * Row arrays (x, y, dy, ...) hold float, bfloat16 or float16 values (`dtype`, one type for all row arrays of a call), start at any
+ * multiple of the value's size and have their rows `ld_...` values apart; weights, states and their gradients are float and
+ * contiguous.  Arithmetic is in float, sums over many rows in double at the end, and no sum depends on the order in which
+ * workgroups finish.  Gradients of weights are added to what is there (accumulate != 0) or written (0); NULL: not wanted. */
+#define TGNN_F32 0
+#define TGNN_BF16 1
+#define TGNN_F16 2
+
+/* Layer norm of every row over its n_cols columns: y = (x - mean) rstd weight + bias with rstd = 1 / sqrt(var + eps) and var the
+ * mean of (x - mean)^2.  weight, bias [n_cols] or NULL (1, 0); out_mean, out_rstd [n_rows] or NULL: what the backward pass
+ * needs.  y may be x itself.  Any n_cols >= 1, n_rows < 2^31 (0: nothing is done). */
+int32_t tgnn_layer_norm_fwd(int32_t dtype, int64_t n_rows, int32_t n_cols, const void* x, int64_t ld_x, const float* weight,
+                            const float* bias, float eps, void* y, int64_t ld_y, float* out_mean, float* out_rstd, void* stream);
+/* Its gradients: with xh = (x - mean) rstd and g = dy weight, dx = rstd (g - mean(g) - xh mean(g xh)), d_weight = sum over the rows
+ * of dy xh, d_bias = sum of dy.  dx may be dy itself, not x.  Without rows d_weight and d_bias are zero (or keep what is there). */
+int64_t tgnn_layer_norm_workspace_bytes(int64_t n_rows, int32_t n_cols);
+int32_t tgnn_layer_norm_bwd(int32_t dtype, int64_t n_rows, int32_t n_cols, const void* dy, int64_t ld_dy, const void* x, int64_t ld_x,
+                            const float* mean, const float* rstd, const float* weight, void* dx, int64_t ld_dx, float* d_weight,
+                            float* d_bias, int32_t accumulate, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Global gradient norm over a list of tensors, and clipping.  g, numel, dtype (and out): HOST arrays [n_tensors] of DEVICE
+ * pointers, numbers of elements and types, which may differ from tensor to tensor; tensors are contiguous, aligned to their type, and may be
+ * empty.  out_norm: device scalar, sqrt of the sum of all squares (formed in double: finite as long as every gradient is, up to
+ * what a float holds).
+ * tgnn_clip_grads then writes out[i] = g[i] * max_norm / norm if norm > max_norm, else g[i]; out = NULL: in place, and g is
+ * left alone where nothing is to be scaled.  max_norm > 0.  A norm that is infinite or not a number scales nothing.
+ * Tensors that are written share no memory with any other of the call (TGNN_E_INVALID_ARG); out[i] may be g[i]. */
+int64_t tgnn_clip_workspace_bytes(int32_t n_tensors);
+int32_t tgnn_grad_norm(int32_t n_tensors, const void* const* g, const int64_t* numel, const int32_t* dtype, float* out_norm,
+                       void* workspace, int64_t workspace_bytes, void* stream);
+int32_t tgnn_clip_grads(int32_t n_tensors, void* const* g, const int64_t* numel, const int32_t* dtype, float max_norm,
+                        void* const* out, float* out_norm, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* A plain streaming copy kernel (dst[i] = src[i], 16-byte words; n_bytes % 16 == 0; buffers must not overlap).
  * It moves a known number of bytes, which calibrates hardware HBM-traffic counters. */
 int32_t tgnn_debug_copy(void* dst, const void* src, int64_t n_bytes, void* stream);

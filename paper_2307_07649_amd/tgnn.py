@@ -54,6 +54,7 @@ class tgnn_batch(C.Structure):
 
 _P = C.c_void_p
 _I = C.c_int32
+_L = C.c_int64
 _SIGS = {
     "tgnn_last_error": (C.c_char_p, []),
     "tgnn_create": (_I, [C.POINTER(tgnn_config), C.POINTER(_P)]),
@@ -86,6 +87,12 @@ _SIGS = {
     "tgnn_debug_read": (_I, [_P, _I, _P, C.c_int64, _P]),
     "tgnn_debug_copy": (_I, [_P, _P, C.c_int64, _P]),
     "tgnn_zero_params": (_I, [_P, C.POINTER(tgnn_params), _P]),
+    "tgnn_layer_norm_fwd": (_I, [_I, _L, _I, _P, _L, _P, _P, C.c_float, _P, _L, _P, _P, _P]),
+    "tgnn_layer_norm_workspace_bytes": (_L, [_L, _I]),
+    "tgnn_layer_norm_bwd": (_I, [_I, _L, _I, _P, _L, _P, _L, _P, _P, _P, _P, _L, _P, _P, _I, _P, _L, _P]),
+    "tgnn_clip_workspace_bytes": (_L, [_I]),
+    "tgnn_grad_norm": (_I, [_I, _P, _P, _P, _P, _P, _L, _P]),
+    "tgnn_clip_grads": (_I, [_I, _P, _P, _P, C.c_float, _P, _P, _P, _L, _P]),
     "tgnn_profile_enable": (_I, [_P, C.c_uint32]),
     "tgnn_profile_every": (_I, [_P, _I]),
     "tgnn_profile_read": (_I, [_P, _I, C.POINTER(_I), C.POINTER(C.c_double)]),
@@ -145,6 +152,114 @@ def tgnn_memory_writeback_noalloc(st, src, dst, eid, t, s_src, s_dst, tau_src, t
                                               src.numel(), _ptr(s_src), _ptr(s_dst), _ptr(tau_src), _ptr(tau_dst),
                                               _ptr(out_winner), _stream()))
     return out_winner
+
+
+# ---- operators on sequences of events: plain functions, no context ----
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _on_device(t, name):
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}: a tensor on the current GPU is needed")
+
+
+def _rows(t, name, like=None, cols=None):
+    """(pointer, row distance) of a row array: two dimensions, values of a row next to each other."""
+    if t.dim() != 2 or t.dtype not in _DTYPES:
+        raise ValueError(f"{name}: a two-dimensional tensor of float32, bfloat16 or float16 is needed, not {tuple(t.shape)} {t.dtype}")
+    if like is not None and (t.dtype != like.dtype or t.shape[0] != like.shape[0] or t.shape[1] != (cols or like.shape[1])):
+        raise ValueError(f"{name}: {(like.shape[0], cols or like.shape[1])} {like.dtype} is needed, not {tuple(t.shape)} {t.dtype}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the values of a row have to be contiguous")
+    _on_device(t, name)
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+
+
+def _floats(t, name, shape):
+    """Pointer of a contiguous float32 tensor of this shape, None for None."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous float32 tensor {tuple(shape)} is needed, not {tuple(t.shape)} {t.dtype}")
+    _on_device(t, name)
+    return t.data_ptr()
+
+
+def _workspace(n_bytes, device):
+    return torch.empty(n_bytes, dtype=torch.uint8, device=device)
+
+
+def _weight_grads(given, shapes, device):
+    """Gradient tensors of weights and whether they are added to: the caller's (all of them or none), or new ones."""
+    n = sum(g is not None for g in given)
+    if n == 0:
+        return [torch.empty(s, dtype=torch.float32, device=device) for s in shapes], 0
+    if n != len(given):
+        raise ValueError("the gradients of all weights are needed, or of none")
+    return list(given), 1
+
+
+def tgnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None):
+    """x [rows, cols], float32, bfloat16 or float16; weight, bias: float32 [cols] or None -> y, mean, rstd."""
+    px, ldx = _rows(x, "x")
+    n, c = x.shape
+    y = torch.empty(n, c, dtype=x.dtype, device=x.device) if out is None else out
+    py, ldy = _rows(y, "out", like=x)
+    mean, rstd = torch.empty(2, n, dtype=torch.float32, device=x.device).unbind(0)
+    _check(_lib.tgnn_layer_norm_fwd(_DTYPES[x.dtype], n, c, px, ldx, _floats(weight, "weight", (c,)), _floats(bias, "bias", (c,)), eps,
+                                    py, ldy, mean.data_ptr(), rstd.data_ptr(), _stream()))
+    return y, mean, rstd
+
+
+def tgnn_layer_norm_bwd(dy, x, mean, rstd, weight=None, d_weight=None, d_bias=None, out=None):
+    """-> dx, d_weight, d_bias.  Given d_weight and d_bias are added to; without them new ones are written."""
+    px, ldx = _rows(x, "x")
+    pdy, lddy = _rows(dy, "dy", like=x)
+    n, c = x.shape
+    dx = torch.empty(n, c, dtype=x.dtype, device=x.device) if out is None else out
+    pdx, lddx = _rows(dx, "out", like=x)
+    (dw, db), add = _weight_grads((d_weight, d_bias), ((c,), (c,)), x.device)
+    ws = _workspace(_lib.tgnn_layer_norm_workspace_bytes(n, c), x.device)
+    _check(_lib.tgnn_layer_norm_bwd(_DTYPES[x.dtype], n, c, pdy, lddy, px, ldx, _floats(mean, "mean", (n,)), _floats(rstd, "rstd", (n,)),
+                                    _floats(weight, "weight", (c,)), pdx, lddx, _floats(dw, "d_weight", (c,)),
+                                    _floats(db, "d_bias", (c,)), add, ws.data_ptr(), ws.numel(), _stream()))
+    return dx, dw, db
+
+
+def _tensor_list(tensors, name):
+    """Host arrays (pointers, numbers of elements, types) of a list of contiguous tensors or of a Params set."""
+    ts = list(tensors.t.values()) if isinstance(tensors, Params) else list(tensors)
+    for t in ts:
+        if t.dtype not in _DTYPES or not t.is_contiguous():
+            raise ValueError(f"{name}: contiguous tensors of float32, bfloat16 or float16 are needed, not {tuple(t.shape)} {t.dtype}")
+        _on_device(t, name)
+    n = len(ts)
+    return ts, (_P * n)(*[t.data_ptr() or None for t in ts]), (_L * n)(*[t.numel() for t in ts]), (_I * n)(*[_DTYPES[t.dtype] for t in ts])
+
+
+def tgnn_grad_norm(grads, out_norm=None):
+    """grads: a list of tensors, or a Params set -> the square root of the sum of all their squares, float32 [1]."""
+    ts, ptr, numel, dtype = _tensor_list(grads, "grads")
+    norm = torch.empty(1, dtype=torch.float32, device=ts[0].device if ts else "cuda") if out_norm is None else out_norm
+    ws = _workspace(_lib.tgnn_clip_workspace_bytes(len(ts)), norm.device)
+    _check(_lib.tgnn_grad_norm(len(ts), ptr, numel, dtype, _floats(norm, "out_norm", (1,)), ws.data_ptr(), ws.numel(), _stream()))
+    return norm
+
+
+def tgnn_clip_grads(grads, max_norm, out=None, out_norm=None):
+    """Scales the gradients to a global norm of at most max_norm, in place or into `out` (tensors of the same sizes and types)
+    -> their norm before, float32 [1]."""
+    ts, ptr, numel, dtype = _tensor_list(grads, "grads")
+    to = None
+    if out is not None:
+        os_, to, n_out, dt_out = _tensor_list(out, "out")
+        if len(os_) != len(ts) or list(n_out) != list(numel) or list(dt_out) != list(dtype):
+            raise ValueError("out: tensors of the gradients' sizes and types are needed")
+    norm = torch.empty(1, dtype=torch.float32, device=ts[0].device if ts else "cuda") if out_norm is None else out_norm
+    ws = _workspace(_lib.tgnn_clip_workspace_bytes(len(ts)), norm.device)
+    _check(_lib.tgnn_clip_grads(len(ts), ptr, numel, dtype, max_norm, to, _floats(norm, "out_norm", (1,)), ws.data_ptr(), ws.numel(),
+                                _stream()))
+    return norm
 
 
 class Graph:
