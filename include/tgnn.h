@@ -373,6 +373,86 @@ int32_t tgnn_profile_read(tgnn_ctx* ctx, int32_t stage, int32_t* out_count, doub
 #define TGNN_BF16 1
 #define TGNN_F16 2
 
+#define TGNN_MAX_SEQ_WIDTH 65536  /* columns of a causal convolution or selective scan */
+#define TGNN_MAX_CONV_WIDTH 8     /* taps of a causal convolution */
+#define TGNN_MAX_SCAN_STATES 64   /* states of a column of a selective scan */
+
+/* Sequences of events as rows of row arrays.  Sequence s < n_seqs has a slot of rows, [indptr[s], indptr[s + 1]) or, with
+ * indptr = NULL, [s max_len, (s + 1) max_len), and the first cnt[s] rows of it (cnt = NULL: all of them) are its events: in time
+ * order, or with newest_first = 1 the most recent one first, as tgnn_sample_recent hands out its [n_roots, k] lists with
+ * their counts.  Rows of a slot behind the count are padding: never read, and zero in every row array that a call
+ * writes.  Rows outside all slots are neither read nor written.  A sequence may be empty.
+ * The device arrays cannot be checked by the host: indptr has to ascend (slots that overlap give meaningless values in the rows they share); a slot
+ * that does not lie within [0, n_rows) is taken as empty, a count that is negative or larger than the slot as zero, so that no
+ * access leaves the arrays.  With indptr, max_len says how long the longest sequence is; only the speed depends on that. */
+typedef struct {
+  const int64_t* indptr; /* [n_seqs + 1] or NULL */
+  const int32_t* cnt;    /* [n_seqs] or NULL */
+  int64_t n_rows;        /* rows of every row array; n_rows < 2^34 */
+  int32_t n_seqs, max_len, newest_first;
+} tgnn_seqs;
+
+/* States (of both operators) are arrays [n_states, ...]; sequence or row s uses state state_idx[s], or state s with
+ * state_idx = NULL (a node's id, for instance).  An index outside [0, n_states) means no state: the sequence starts from zero and its end is not
+ * kept.  state_in NULL: all start from zero; state_out NULL: no end is kept.  Entries of state_out that no sequence refers to stay as they are;
+ * indexes inside [0, n_states) have to differ from each other (of two equal ones it is not defined which end is kept).  Over sequences
+ * state_out must not overlap state_in; the single-event forms may update in place.  States are constants in the backward passes
+ * (no back-propagation through a stored state, as with node memory). */
+
+/* Short causal convolution along every sequence, one filter per column: pre[t, c] = bias[c] + sum over j < width of
+ * weight[c, j] x[t - (width - 1) + j, c] with the state's rows (the width - 1 inputs before the first event, oldest first, in the row
+ * arrays' type: [n_states, width - 1, d], contiguous) or zeros in front; y = silu(pre) = pre / (1 + exp(-pre)) with silu != 0,
+ * else pre.  weight [d, width], bias [d] or NULL.  1 <= width <= TGNN_MAX_CONV_WIDTH.  y must not overlap x. */
+int32_t tgnn_causal_conv_fwd(const tgnn_seqs* seqs, int32_t dtype, int32_t d, int32_t width, const void* x, int64_t ld_x,
+                             const float* weight, const float* bias, int32_t silu, const void* state_in, void* state_out,
+                             const int32_t* state_idx, int32_t n_states, void* y, int64_t ld_y, void* stream);
+/* One event for each of n_rows sequences: row i follows on state state_idx[i] (or i).  state_out may be state_in, y may be x. */
+int32_t tgnn_causal_conv_step(int32_t dtype, int64_t n_rows, int32_t d, int32_t width, const void* x, int64_t ld_x,
+                              const float* weight, const float* bias, int32_t silu, const void* state_in, void* state_out,
+                              const int32_t* state_idx, int32_t n_states, void* y, int64_t ld_y, void* stream);
+/* Gradients for dy; x and the state as in the forward call.  dx must not overlap x or dy. */
+int64_t tgnn_causal_conv_workspace_bytes(int32_t d, int32_t width);
+int32_t tgnn_causal_conv_bwd(const tgnn_seqs* seqs, int32_t dtype, int32_t d, int32_t width, const void* dy, int64_t ld_dy,
+                             const void* x, int64_t ld_x, const float* weight, const float* bias, int32_t silu,
+                             const void* state_in, const int32_t* state_idx, int32_t n_states, void* dx, int64_t ld_dx,
+                             float* d_weight, float* d_bias, int32_t accumulate, void* workspace, int64_t workspace_bytes,
+                             void* stream);
+
+/* Selective state space scan.  Column c has n_state states h, its step size, input and output weights come with the event:
+ *   delta = softplus(dt + dt_bias) (dt + dt_bias with softplus = 0),  h[n] = exp(delta A[c, n]) h[n] + delta x B[g, n],
+ *   y = (sum over n of C[g, n] h[n] + D[c] x) silu(z)
+ * with g = c / (d / n_groups) the column's group.  dt_bias, D NULL: zero; z NULL: no gate. */
+typedef struct {
+  int32_t dtype, d, n_state, n_groups, softplus, n_states;
+  const void *x, *dt, *B, *C, *z;             /* [rows, d] x 2, [rows, n_groups n_state] x 2, [rows, d] */
+  int64_t ld_x, ld_dt, ld_b, ld_c, ld_z;
+  const float *A, *D, *dt_bias;               /* [d, n_state], [d], [d] */
+  const float* state_in;                      /* [n_states, d, n_state] */
+  const int32_t* state_idx;
+} tgnn_scan;
+/* The gradients of tgnn_selective_scan_bwd: row arrays like the inputs' (dz only with z), and of the weights. */
+typedef struct {
+  void *dx, *ddt, *dB, *dC, *dz;
+  int64_t ld_dx, ld_ddt, ld_db, ld_dc, ld_dz;
+  float *dA, *dD, *ddt_bias;
+} tgnn_scan_grads;
+
+/* Sizes: of `saved`, which a forward call fills for its backward call (states every 32 events), and of the workspace of a forward (backward = 0)
+ * or backward call (saved != 0: with `saved` at hand).  Negative: an error, as everywhere. */
+int64_t tgnn_selective_scan_saved_bytes(const tgnn_seqs* seqs, int32_t d, int32_t n_state);
+int64_t tgnn_selective_scan_workspace_bytes(const tgnn_seqs* seqs, int32_t d, int32_t n_state, int32_t n_groups, int32_t backward,
+                                            int32_t saved);
+/* state_out [n_states, d, n_state] or NULL; saved or NULL: nothing is kept for a backward call.  y must not overlap an input. */
+int32_t tgnn_selective_scan_fwd(const tgnn_seqs* seqs, const tgnn_scan* scan, void* y, int64_t ld_y, float* state_out, float* saved,
+                                int64_t saved_bytes, void* workspace, int64_t workspace_bytes, void* stream);
+/* One event for each of n_rows sequences; state_out may be scan->state_in. */
+int32_t tgnn_selective_scan_step(const tgnn_scan* scan, int64_t n_rows, void* y, int64_t ld_y, float* state_out, void* stream);
+/* Gradients for dy; the inputs as in the forward call.  saved NULL: the states are formed again.  No gradient array may overlap an input.  The gradient
+ * of a row's step size is that of dt (through the softplus), ddt_bias is its sum over all rows of sequences. */
+int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_scan* scan, const void* dy, int64_t ld_dy, const float* saved,
+                                int64_t saved_bytes, const tgnn_scan_grads* grads, int32_t accumulate, void* workspace,
+                                int64_t workspace_bytes, void* stream);
+
 /* Layer norm of every row over its n_cols columns: y = (x - mean) rstd weight + bias with rstd = 1 / sqrt(var + eps) and var the
  * mean of (x - mean)^2.  weight, bias [n_cols] or NULL (1, 0); out_mean, out_rstd [n_rows] or NULL: what the backward pass
  * needs.  y may be x itself.  Any n_cols >= 1, n_rows < 2^31 (0: nothing is done). */

@@ -52,6 +52,24 @@ class tgnn_batch(C.Structure):
                 ("t", C.c_void_p), ("n", C.c_int32), ("replica", C.c_int32)]
 
 
+class tgnn_seqs(C.Structure):
+    _fields_ = [("indptr", C.c_void_p), ("cnt", C.c_void_p), ("n_rows", C.c_int64), ("n_seqs", C.c_int32), ("max_len", C.c_int32),
+                ("newest_first", C.c_int32)]
+
+
+class tgnn_scan(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "d", "n_state", "n_groups", "softplus", "n_states")] +
+                [(n, C.c_void_p) for n in ("x", "dt", "B", "C", "z")] +
+                [(n, C.c_int64) for n in ("ld_x", "ld_dt", "ld_b", "ld_c", "ld_z")] +
+                [(n, C.c_void_p) for n in ("A", "D", "dt_bias", "state_in", "state_idx")])
+
+
+class tgnn_scan_grads(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("dx", "ddt", "dB", "dC", "dz")] +
+                [(n, C.c_int64) for n in ("ld_dx", "ld_ddt", "ld_db", "ld_dc", "ld_dz")] +
+                [(n, C.c_void_p) for n in ("dA", "dD", "ddt_bias")])
+
+
 _P = C.c_void_p
 _I = C.c_int32
 _L = C.c_int64
@@ -87,6 +105,17 @@ _SIGS = {
     "tgnn_debug_read": (_I, [_P, _I, _P, C.c_int64, _P]),
     "tgnn_debug_copy": (_I, [_P, _P, C.c_int64, _P]),
     "tgnn_zero_params": (_I, [_P, C.POINTER(tgnn_params), _P]),
+    "tgnn_causal_conv_fwd": (_I, [C.POINTER(tgnn_seqs), _I, _I, _I, _P, _L, _P, _P, _I, _P, _P, _P, _I, _P, _L, _P]),
+    "tgnn_causal_conv_step": (_I, [_I, _L, _I, _I, _P, _L, _P, _P, _I, _P, _P, _P, _I, _P, _L, _P]),
+    "tgnn_causal_conv_workspace_bytes": (_L, [_I, _I]),
+    "tgnn_causal_conv_bwd": (_I, [C.POINTER(tgnn_seqs), _I, _I, _I, _P, _L, _P, _L, _P, _P, _I, _P, _P, _I, _P, _L, _P, _P, _I, _P,
+                                  _L, _P]),
+    "tgnn_selective_scan_saved_bytes": (_L, [C.POINTER(tgnn_seqs), _I, _I]),
+    "tgnn_selective_scan_workspace_bytes": (_L, [C.POINTER(tgnn_seqs), _I, _I, _I, _I, _I]),
+    "tgnn_selective_scan_fwd": (_I, [C.POINTER(tgnn_seqs), C.POINTER(tgnn_scan), _P, _L, _P, _P, _L, _P, _L, _P]),
+    "tgnn_selective_scan_step": (_I, [C.POINTER(tgnn_scan), _L, _P, _L, _P, _P]),
+    "tgnn_selective_scan_bwd": (_I, [C.POINTER(tgnn_seqs), C.POINTER(tgnn_scan), _P, _L, _P, _L, C.POINTER(tgnn_scan_grads), _I, _P,
+                                     _L, _P]),
     "tgnn_layer_norm_fwd": (_I, [_I, _L, _I, _P, _L, _P, _P, C.c_float, _P, _L, _P, _P, _P]),
     "tgnn_layer_norm_workspace_bytes": (_L, [_L, _I]),
     "tgnn_layer_norm_bwd": (_I, [_I, _L, _I, _P, _L, _P, _L, _P, _P, _P, _P, _L, _P, _P, _I, _P, _L, _P]),
@@ -169,7 +198,7 @@ def _rows(t, name, like=None, cols=None):
         raise ValueError(f"{name}: a two-dimensional tensor of float32, bfloat16 or float16 is needed, not {tuple(t.shape)} {t.dtype}")
     if like is not None and (t.dtype != like.dtype or t.shape[0] != like.shape[0] or t.shape[1] != (cols or like.shape[1])):
         raise ValueError(f"{name}: {(like.shape[0], cols or like.shape[1])} {like.dtype} is needed, not {tuple(t.shape)} {t.dtype}")
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    if t.shape[0] > 0 and t.shape[1] > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: the values of a row have to be contiguous")
     _on_device(t, name)
     return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
@@ -197,6 +226,177 @@ def _weight_grads(given, shapes, device):
     if n != len(given):
         raise ValueError("the gradients of all weights are needed, or of none")
     return list(given), 1
+
+
+class Seqs:
+    """Sequences of events as rows of row arrays (tgnn_seqs): indptr int64 [n_seqs + 1] or None (slots of max_len rows), cnt
+    int32 [n_seqs] or None (slots are full); newest_first: rows as tgnn_sample_recent orders them.  max_len: rows of a slot, or with
+    indptr the length of the longest sequence."""
+
+    def __init__(self, n_rows, n_seqs, max_len, indptr=None, cnt=None, newest_first=False):
+        for t, name, dtype, n in ((indptr, "indptr", torch.int64, n_seqs + 1), (cnt, "cnt", torch.int32, n_seqs)):
+            if t is not None:
+                if t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous():
+                    raise ValueError(f"{name}: a contiguous {dtype} tensor ({n},) is needed, not {tuple(t.shape)} {t.dtype}")
+                _on_device(t, name)
+        self.indptr, self.cnt, self.n_rows = indptr, cnt, n_rows
+        self.c = tgnn_seqs(None if indptr is None else indptr.data_ptr(), None if cnt is None else cnt.data_ptr(), n_rows, n_seqs,
+                           max_len, 1 if newest_first else 0)
+
+
+def _seq_rows(seqs, x):
+    if x.dim() == 2 and x.shape[0] != seqs.n_rows:
+        raise ValueError(f"x has {x.shape[0]} rows, the sequences {seqs.n_rows}")
+
+
+def _states(state_in, state_out, state_idx, n, shape, dtype):
+    """(state_in, state_out, state_idx, n_states) as the library takes them; n: sequences (or rows) of the call."""
+    given = [(t, name) for t, name in ((state_in, "state_in"), (state_out, "state_out")) if t is not None]
+    for t, name in given:
+        if t.dtype != dtype or tuple(t.shape[1:]) != shape or t.dim() != 3 or not t.is_contiguous() or t.shape[0] != given[0][0].shape[0]:
+            raise ValueError(f"{name}: a contiguous {dtype} tensor {('n_states',) + shape} is needed, not {tuple(t.shape)} {t.dtype}")
+        _on_device(t, name)
+    if state_idx is not None:
+        if state_idx.dtype != torch.int32 or tuple(state_idx.shape) != (n,) or not state_idx.is_contiguous():
+            raise ValueError(f"state_idx: a contiguous int32 tensor ({n},) is needed, not {tuple(state_idx.shape)} {state_idx.dtype}")
+        _on_device(state_idx, "state_idx")
+    elif given and given[0][0].shape[0] != n:
+        raise ValueError(f"{given[0][1]}: {n} states are needed without state_idx, not {given[0][0].shape[0]}")
+    ptr = [None if t is None else t.data_ptr() for t in (state_in, state_out, state_idx)]
+    return (*ptr, given[0][0].shape[0] if given else 0)
+
+
+def tgnn_causal_conv_fwd(seqs, x, weight, bias=None, silu=True, state_in=None, state_out=None, state_idx=None, out=None):
+    """x [rows, d], float32, bfloat16 or float16; weight [d, width], bias [d] float32; states [n_states, width - 1, d] in x's type
+    -> y (without `out` a new tensor, in which rows outside all slots hold nothing in particular)."""
+    _seq_rows(seqs, x)
+    px, ldx = _rows(x, "x")
+    d, w = x.shape[1], weight.shape[-1]
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    py, ldy = _rows(y, "out", like=x)
+    si, so, ix, ns = _states(state_in, state_out, state_idx, seqs.c.n_seqs, (w - 1, d), x.dtype)
+    _check(_lib.tgnn_causal_conv_fwd(seqs.c, _DTYPES[x.dtype], d, w, px, ldx, _floats(weight, "weight", (d, w)),
+                                     _floats(bias, "bias", (d,)), 1 if silu else 0, si, so, ix, ns, py, ldy, _stream()))
+    return y
+
+
+def tgnn_causal_conv_step(x, weight, bias=None, silu=True, state_in=None, state_out=None, state_idx=None, out=None):
+    """One event per row of x; state_out may be state_in -> y."""
+    px, ldx = _rows(x, "x")
+    n, d = x.shape
+    w = weight.shape[-1]
+    y = torch.empty(n, d, dtype=x.dtype, device=x.device) if out is None else out
+    py, ldy = _rows(y, "out", like=x)
+    si, so, ix, ns = _states(state_in, state_out, state_idx, n, (w - 1, d), x.dtype)
+    _check(_lib.tgnn_causal_conv_step(_DTYPES[x.dtype], n, d, w, px, ldx, _floats(weight, "weight", (d, w)), _floats(bias, "bias", (d,)),
+                                      1 if silu else 0, si, so, ix, ns, py, ldy, _stream()))
+    return y
+
+
+def tgnn_causal_conv_bwd(seqs, dy, x, weight, bias=None, silu=True, state_in=None, state_idx=None, d_weight=None, d_bias=None,
+                         out=None):
+    """-> dx, d_weight, d_bias.  Given d_weight and d_bias are added to; without them new ones are written."""
+    _seq_rows(seqs, x)
+    px, ldx = _rows(x, "x")
+    pdy, lddy = _rows(dy, "dy", like=x)
+    d, w = x.shape[1], weight.shape[-1]
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    pdx, lddx = _rows(dx, "out", like=x)
+    (dw, db), add = _weight_grads((d_weight, d_bias), ((d, w), (d,)), x.device)
+    si, _, ix, ns = _states(state_in, None, state_idx, seqs.c.n_seqs, (w - 1, d), x.dtype)
+    ws = _workspace(_lib.tgnn_causal_conv_workspace_bytes(d, w), x.device)
+    _check(_lib.tgnn_causal_conv_bwd(seqs.c, _DTYPES[x.dtype], d, w, pdy, lddy, px, ldx, _floats(weight, "weight", (d, w)),
+                                     _floats(bias, "bias", (d,)), 1 if silu else 0, si, ix, ns, pdx, lddx, _floats(dw, "d_weight", (d, w)),
+                                     _floats(db, "d_bias", (d,)), add, ws.data_ptr(), ws.numel(), _stream()))
+    return dx, dw, db
+
+
+def _scan_args(x, dt, A, B, Cm, D, z, dt_bias, softplus, states):
+    px, ldx = _rows(x, "x")
+    if A.dim() != 2:
+        raise ValueError(f"A: a float32 tensor (d, n_state) is needed, not {tuple(A.shape)} {A.dtype}")
+    d, n = A.shape
+    if x.shape[1] != d or n == 0 or B.dim() != 2 or B.shape[1] % n != 0 or B.shape[1] == 0:
+        raise ValueError(f"x {tuple(x.shape)}, A {tuple(A.shape)} and B {tuple(B.shape)} do not belong together")
+    pdt, lddt = _rows(dt, "dt", like=x)
+    pb, ldb = _rows(B, "B", like=x, cols=B.shape[1])
+    pc, ldc = _rows(Cm, "C", like=x, cols=B.shape[1])
+    pz, ldz = (None, 0) if z is None else _rows(z, "z", like=x)
+    si, _, ix, ns = states
+    return tgnn_scan(_DTYPES[x.dtype], d, n, B.shape[1] // n, 1 if softplus else 0, ns, px, pdt, pb, pc, pz, ldx, lddt, ldb, ldc, ldz,
+                     _floats(A, "A", (d, n)), _floats(D, "D", (d,)), _floats(dt_bias, "dt_bias", (d,)), si, ix)
+
+
+def _bytes(n):
+    if n < 0:
+        raise TgnnError(n)
+    return n
+
+
+def selective_scan_saved(seqs, A):
+    """A buffer that tgnn_selective_scan_fwd fills for tgnn_selective_scan_bwd (the states every 32 events)."""
+    return torch.empty(_bytes(_lib.tgnn_selective_scan_saved_bytes(seqs.c, *A.shape)) // 4, dtype=torch.float32, device=A.device)
+
+
+def _saved(saved):
+    if saved is None:
+        return None, 0
+    return _floats(saved, "saved", saved.shape), saved.numel() * 4
+
+
+def tgnn_selective_scan_fwd(seqs, x, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, state_in=None, state_out=None,
+                            state_idx=None, saved=None, out=None):
+    """x, dt, z [rows, d], B, C [rows, n_groups n_state], float32, bfloat16 or float16; A [d, n_state], D, dt_bias [d] float32;
+    states [n_states, d, n_state] float32; saved: selective_scan_saved(...) -> y (without `out` a new tensor, in which rows outside all
+    slots hold nothing in particular)."""
+    _seq_rows(seqs, x)
+    states = _states(state_in, state_out, state_idx, seqs.c.n_seqs, tuple(A.shape), torch.float32)
+    a = _scan_args(x, dt, A, B, C, D, z, dt_bias, softplus, states)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    py, ldy = _rows(y, "out", like=x)
+    ps, ns = _saved(saved)
+    need = _bytes(_lib.tgnn_selective_scan_workspace_bytes(seqs.c, a.d, a.n_state, a.n_groups, 0, 0))
+    ws = _workspace(need, x.device) if need else None
+    _check(_lib.tgnn_selective_scan_fwd(seqs.c, a, py, ldy, states[1], ps, ns, ws.data_ptr() if need else None, need, _stream()))
+    return y
+
+
+def tgnn_selective_scan_step(x, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, state_in=None, state_out=None,
+                             state_idx=None, out=None):
+    """One event per row; state_out may be state_in -> y."""
+    states = _states(state_in, state_out, state_idx, x.shape[0], tuple(A.shape), torch.float32)
+    a = _scan_args(x, dt, A, B, C, D, z, dt_bias, softplus, states)
+    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    py, ldy = _rows(y, "out", like=x)
+    _check(_lib.tgnn_selective_scan_step(a, x.shape[0], py, ldy, states[1], _stream()))
+    return y
+
+
+def tgnn_selective_scan_bwd(seqs, dy, x, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, state_in=None, state_idx=None,
+                            saved=None, dA=None, dD=None, ddt_bias=None, out=None):
+    """-> dict of dx, ddt, dB, dC, dA and, with z, D, dt_bias given, dz, dD, ddt_bias.  Given gradients of the weights (of all
+    that there are) are added to; without them new ones are written.  out: a dict of the row arrays to write (dx, ddt, dB, dC, dz)."""
+    _seq_rows(seqs, x)
+    states = _states(state_in, None, state_idx, seqs.c.n_seqs, tuple(A.shape), torch.float32)
+    a = _scan_args(x, dt, A, B, C, D, z, dt_bias, softplus, states)
+    pdy, lddy = _rows(dy, "dy", like=x)
+    names = ["dA"] + ["dD"] * (D is not None) + ["ddt_bias"] * (dt_bias is not None)
+    given = dict(dA=dA, dD=dD, ddt_bias=ddt_bias)
+    if any(g is not None and n not in names for n, g in given.items()):
+        raise ValueError("a gradient of a weight that there is none of")
+    w, add = _weight_grads([given[n] for n in names], [tuple(A.shape) if n == "dA" else (a.d,) for n in names], x.device)
+    like = dict(dx=x, ddt=x, dB=B, dC=B, dz=z)
+    g = {n: torch.empty(v.shape, dtype=x.dtype, device=x.device) if out is None else out[n] for n, v in like.items() if v is not None}
+    rows = [(None, 0) if v is None else _rows(g[n], n, like=v) for n, v in like.items()]
+    g.update(zip(names, w))
+    c = tgnn_scan_grads(*[r[0] for r in rows], *[r[1] for r in rows],
+                        _floats(g["dA"], "dA", tuple(A.shape)), _floats(g.get("dD"), "dD", (a.d,)),
+                        _floats(g.get("ddt_bias"), "ddt_bias", (a.d,)))
+    ps, ns = _saved(saved)
+    need = _bytes(_lib.tgnn_selective_scan_workspace_bytes(seqs.c, a.d, a.n_state, a.n_groups, 1, 0 if saved is None else 1))
+    ws = _workspace(need, x.device)
+    _check(_lib.tgnn_selective_scan_bwd(seqs.c, a, pdy, lddy, ps, ns, c, add, ws.data_ptr(), need, _stream()))
+    return g
 
 
 def tgnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None):

@@ -92,3 +92,135 @@ def test_the_binding_refuses_what_it_cannot_hand_over(tgnn):
         tgnn.tgnn_grad_norm([torch.zeros(8, 4).t()])
     with pytest.raises(ValueError, match="current GPU"):
         tgnn.tgnn_clip_grads([x], 1.0)
+
+
+def make_seqs(tgnn, n_rows=40, n_seqs=4, max_len=10, indptr=None, cnt=None, newest_first=0):
+    return tgnn.tgnn_seqs(indptr, cnt, n_rows, n_seqs, max_len, newest_first)
+
+
+CONV = (["seqs", "dtype", "d", "width", "x", "ld_x", "weight", "bias", "silu", "state_in", "state_out", "state_idx", "n_states", "y", "ld_y", "stream"],
+        [None, 0, 8, 4, P, 8, S, S, 1, Q, R, None, 4, S + 4096, 8, None])
+STEP = (["dtype", "rows"] + CONV[0][2:], [0, 4] + CONV[1][2:])
+CONV_BWD = (["seqs", "dtype", "d", "width", "dy", "ld_dy", "x", "ld_x", "weight", "bias", "silu", "state_in", "state_idx", "n_states", "dx", "ld_dx", "dw",
+             "db", "acc", "ws", "ws_bytes", "stream"],
+            [None, 0, 8, 4, P, 8, Q, 8, S, S, 1, S + 8192, None, 4, R, 8, S, S, 0, S, 1 << 20, None])
+
+SEQS_BAD = [(dict(n_seqs=-1), INVALID, "negative"), (dict(max_len=-1), INVALID, "negative"), (dict(n_rows=-1), INVALID, "negative"),
+            (dict(newest_first=2), INVALID, "newest_first"), (dict(indptr=P + 4), MISALIGNED, "indptr"), (dict(cnt=P + 2), MISALIGNED, "cnt"),
+            (dict(max_len=11), RANGE, "do not fit"), (dict(n_rows=1 << 34, indptr=P), RANGE, "rows")]
+
+
+@pytest.mark.parametrize("seqs,code,word", SEQS_BAD)
+def test_sequences(tgnn, seqs, code, word):
+    for name, (names, args) in (("tgnn_causal_conv_fwd", CONV), ("tgnn_causal_conv_bwd", CONV_BWD)):
+        rc, msg = call(tgnn, name, args, names, seqs=make_seqs(tgnn, **seqs))
+        assert rc == code and word in msg, (name, rc, msg)
+    q = make_seqs(tgnn, **seqs)
+    p = make_scan(tgnn)
+    assert tgnn._lib.tgnn_selective_scan_fwd(q, p, R, 8, None, None, 0, S, 1 << 20, None) == code
+    assert tgnn._lib.tgnn_selective_scan_bwd(q, p, P, 8, None, 0, make_grads(tgnn), 0, S, 1 << 20, None) == code
+    assert tgnn._lib.tgnn_selective_scan_saved_bytes(q, 8, 4) == code
+    assert tgnn._lib.tgnn_selective_scan_workspace_bytes(q, 8, 4, 1, 0, 0) == code
+
+
+CONV_BAD = [(dict(dtype=9), INVALID, "dtype"), (dict(d=0), DIM, "d = 0"), (dict(d=65537), DIM, "d ="), (dict(width=0), DIM, "width"), (dict(width=9), DIM, "width"),
+            (dict(weight=None), NULL, "weight"), (dict(weight=S + 2), MISALIGNED, "weight"), (dict(x=None), NULL, "x"), (dict(ld_x=7), INVALID, "rows of x"),
+            (dict(n_states=-1), INVALID, "n_states"), (dict(state_in=Q + 2), MISALIGNED, "state"), (dict(state_idx=P + 1), MISALIGNED, "state_idx")]
+
+
+@pytest.mark.parametrize("over,code,word", CONV_BAD + [
+    (dict(y=None), NULL, "y"), (dict(ld_y=2), INVALID, "rows of y"), (dict(y=P), INVALID, "y overlaps x"), (dict(state_out=Q), INVALID, "state_out overlaps"),
+    (dict(state_out=Q + 4 * 3 * 8 * 4 - 4), INVALID, "state_out overlaps")])
+def test_conv_fwd(tgnn, over, code, word):
+    rc, msg = call(tgnn, "tgnn_causal_conv_fwd", CONV[1], CONV[0], **{"seqs": make_seqs(tgnn), **over})
+    assert rc == code and word in msg, (rc, msg)
+    assert call(tgnn, "tgnn_causal_conv_fwd", CONV[1], CONV[0], seqs=None)[0] == NULL
+
+
+@pytest.mark.parametrize("over,code,word", CONV_BAD + [
+    (dict(rows=-1), RANGE, "n_rows"), (dict(rows=1 << 31), RANGE, "n_rows"), (dict(y=P + 4), INVALID, "without being it"), (dict(y=P, ld_y=9), INVALID, "without being it"),
+    (dict(state_out=Q + 4), INVALID, "without being it")])
+def test_conv_step(tgnn, over, code, word):
+    rc, msg = call(tgnn, "tgnn_causal_conv_step", STEP[1], STEP[0], **over)
+    assert rc == code and word in msg, (rc, msg)
+
+
+@pytest.mark.parametrize("over,code,word", CONV_BAD + [
+    (dict(dy=None), NULL, "dy"), (dict(dx=None), NULL, "dx"), (dict(dx=Q), INVALID, "overlaps"), (dict(dx=P), INVALID, "overlaps"), (dict(ws=None), NULL, "workspace"),
+    (dict(ws=S + 4), MISALIGNED, "workspace"), (dict(ws_bytes=8), WORKSPACE, "needed"), (dict(dw=S + 1), MISALIGNED, "d_weight")])
+def test_conv_bwd(tgnn, over, code, word):
+    rc, msg = call(tgnn, "tgnn_causal_conv_bwd", CONV_BWD[1], CONV_BWD[0], **{"seqs": make_seqs(tgnn), **over})
+    assert rc == code and word in msg, (rc, msg)
+
+
+def make_scan(tgnn, **over):
+    v = dict(dtype=0, d=8, n_state=4, n_groups=2, softplus=1, n_states=4, x=P, dt=P, B=P, C=P, z=P, ld_x=8, ld_dt=8, ld_b=8, ld_c=8, ld_z=8, A=Q, D=Q, dt_bias=Q,
+             state_in=Q, state_idx=None)
+    assert not set(over) - set(v)
+    return tgnn.tgnn_scan(**{**v, **over})
+
+
+def make_grads(tgnn, **over):
+    v = dict(dx=R, ddt=R, dB=R, dC=R, dz=R, ld_dx=8, ld_ddt=8, ld_db=8, ld_dc=8, ld_dz=8, dA=S, dD=S, ddt_bias=S)
+    return tgnn.tgnn_scan_grads(**{**v, **over})
+
+
+@pytest.mark.parametrize("over,code,word", [
+    (dict(dtype=-1), INVALID, "dtype"), (dict(d=0), DIM, "d = 0"), (dict(d=65538), DIM, "d ="), (dict(n_state=0), DIM, "n_state"), (dict(n_state=65), DIM, "n_state"),
+    (dict(n_groups=3), DIM, "groups"), (dict(n_groups=0), DIM, "groups"), (dict(x=None), NULL, "x"), (dict(dt=None), NULL, "dt"), (dict(B=None), NULL, "B"),
+    (dict(C=None), NULL, "C"), (dict(A=None), NULL, "A"), (dict(A=Q + 1), MISALIGNED, "A"), (dict(z=P + 2), MISALIGNED, "z"), (dict(ld_b=7), INVALID, "rows of B"),
+    (dict(ld_x=1), INVALID, "rows of x"), (dict(state_in=Q + 2), MISALIGNED, "state_in"), (dict(n_states=-2), INVALID, "n_states")])
+def test_scan_inputs(tgnn, over, code, word):
+    q, p = make_seqs(tgnn), make_scan(tgnn, **over)
+    lib = tgnn._lib
+    for rc in (lib.tgnn_selective_scan_fwd(q, p, R, 8, None, None, 0, S, 1 << 20, None), lib.tgnn_selective_scan_step(p, 4, R, 8, None, None),
+               lib.tgnn_selective_scan_bwd(q, p, P, 8, None, 0, make_grads(tgnn), 0, S, 1 << 20, None)):
+        assert rc == code and word in lib.tgnn_last_error().decode(), (rc, lib.tgnn_last_error())
+
+
+def test_scan_outputs_and_workspaces(tgnn):
+    lib, q, p, g = tgnn._lib, make_seqs(tgnn), make_scan(tgnn), make_grads(tgnn)
+
+    def fwd(y=R, ld=8, so=None, sv=None, svb=0, ws=S, wsb=1 << 20, q=q, p=p):
+        return lib.tgnn_selective_scan_fwd(q, p, y, ld, so, sv, svb, ws, wsb, None)
+    assert fwd(y=None) == NULL and fwd(y=R + 2) == MISALIGNED and fwd(ld=7) == INVALID and fwd(y=P) == INVALID
+    assert fwd(so=Q) == INVALID and fwd(so=Q + 4 * 8 * 4 * 4 - 4) == INVALID and fwd(so=S + 1) == MISALIGNED
+    assert fwd(sv=S + 4) == MISALIGNED and fwd(sv=S, svb=100) == WORKSPACE and fwd(p=None) == NULL and fwd(q=None) == NULL
+    long = make_seqs(tgnn, n_rows=4000, n_seqs=1, max_len=4000)
+    need = lib.tgnn_selective_scan_workspace_bytes(long, 8, 4, 2, 0, 0)
+    assert need > 0 and fwd(q=long, ws=None) == NULL and fwd(q=long, y=R + (1 << 19), ws=S, wsb=need - 1) == WORKSPACE and fwd(q=long, ws=S + 8, wsb=need) == MISALIGNED
+
+    def step(rows=4, y=R, so=None, p=p):
+        return lib.tgnn_selective_scan_step(p, rows, y, 8, so, None)
+    assert step(rows=-1) == RANGE and step(rows=1 << 31) == RANGE and step(y=None) == NULL and step(y=P) == INVALID and step(so=Q + 4) == INVALID
+
+    def bwd(dy=P, sv=None, svb=0, g=g, ws=S, wsb=1 << 20, p=p):
+        return lib.tgnn_selective_scan_bwd(q, p, dy, 8, sv, svb, g, 0, ws, wsb, None)
+    assert bwd(dy=None) == NULL and bwd(g=None) == NULL and bwd(ws=None) == NULL and bwd(ws=S + 4) == MISALIGNED and bwd(wsb=64) == WORKSPACE
+    assert bwd(sv=S + 4) == MISALIGNED and bwd(sv=S, svb=4) == WORKSPACE
+    for k in ("dx", "ddt", "dB", "dC", "dz"):
+        assert bwd(g=make_grads(tgnn, **{k: None})) == NULL and bwd(g=make_grads(tgnn, **{k: P})) == INVALID, k
+    assert bwd(g=make_grads(tgnn, ld_db=3)) == INVALID and bwd(g=make_grads(tgnn, dA=S + 2)) == MISALIGNED
+    assert lib.tgnn_selective_scan_saved_bytes(q, 8, 65) == DIM and lib.tgnn_selective_scan_workspace_bytes(q, 8, 4, 3, 0, 0) == DIM
+
+
+def test_struct_sizes(tgnn):
+    assert C.sizeof(tgnn.tgnn_seqs) == 40 and C.sizeof(tgnn.tgnn_scan) == 24 + 15 * 8 and C.sizeof(tgnn.tgnn_scan_grads) == 13 * 8
+
+
+def test_the_binding_refuses_sequences_and_states_that_do_not_fit(tgnn):
+    with pytest.raises(ValueError, match="indptr"):
+        tgnn.Seqs(10, 2, 5, indptr=torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="cnt"):
+        tgnn.Seqs(10, 2, 5, cnt=torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="current GPU"):
+        tgnn.Seqs(10, 2, 5, cnt=torch.zeros(2, dtype=torch.int32))
+    x, A = torch.zeros(10, 8), torch.zeros(8, 4)
+    q = tgnn.Seqs(10, 2, 5)
+    for bad in (torch.zeros(2, 8, 5), torch.zeros(2, 8, 4, dtype=torch.float64), torch.zeros(2, 4, 8).transpose(1, 2)):
+        with pytest.raises(ValueError, match="state_in"):
+            tgnn.tgnn_selective_scan_fwd(q, x, x, A, x, x, state_in=bad)
+    with pytest.raises(ValueError, match="rows"):
+        tgnn.tgnn_selective_scan_fwd(q, torch.zeros(9, 8), x, A, x, x)
+    with pytest.raises(ValueError, match="rows"):
+        tgnn.tgnn_causal_conv_fwd(q, torch.zeros(9, 8), torch.zeros(8, 4))
