@@ -328,6 +328,7 @@ int check_row_array(const char* name, const void* p, int64_t ld, int64_t rows, i
   if (rows > 0 && p == nullptr) return set_error(TGNN_E_NULL_PTR, "%s is NULL", name);
   if (!aligned_to(p, type_size(dtype))) return set_error(TGNN_E_MISALIGNED, "%s is not aligned to its type", name);
   if (ld < cols) return set_error(TGNN_E_INVALID_ARG, "the rows of %s are %lld apart and %d long", name, (long long)ld, cols);
+  if (ld > (int64_t(1) << 27)) return set_error(TGNN_E_OUT_OF_RANGE, "the rows of %s are %lld apart", name, (long long)ld);
   return TGNN_OK;
 }
 

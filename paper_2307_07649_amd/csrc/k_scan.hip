@@ -71,8 +71,6 @@ __device__ __forceinline__ float softplus(float v) {
 }
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-v * LOG2E)); }
 
-__device__ __forceinline__ float lane_value(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
-
 __device__ __forceinline__ int64_t state_of(const ScanArgs& a, int s) {
   const int64_t i = a.state_idx != nullptr ? a.state_idx[s] : s;
   return i >= 0 && i < a.n_states ? i : -1;
@@ -102,163 +100,210 @@ template <int NP> __device__ __forceinline__ void store_states(float* p, int n, 
   }
 }
 
-enum { SCAN_Y, SCAN_STATES, SCAN_PART };   // outputs; saved states only; a segment's own part
+enum { SCAN_Y, SCAN_STATES, SCAN_PART, SCAN_BACK_PART };   // outputs; saved states only; a segment's own part, forward and backward
 
-// What a wavefront asks for of an event before it needs it
-template <class T> struct Event { T x, dt, z; T b, c; };
+// Four events of a wavefront on their way to the registers: the columns' values, one event per register, and the events' B and C,
+// one value of the 4 x NP per lane (and register)
+template <class T, int NP> struct Events {
+  static constexpr int R = NP > 16 ? NP / 16 : 1;
+  T x[4], dt[4], z[4], b[R], c[R];
+};
 
-// One wavefront: 64 columns of a group over a segment (or a whole sequence).
-template <class T, int NP, int MODE>
+// One wavefront: 64 columns of a group over a segment (or a whole sequence), four events at a time, the next four on their way.  The
+// events' B and C go through a piece of LDS that only this wavefront uses: read back, every lane has all of them (a vector
+// read of the same address for all lanes; taking them lane by lane from a register instead cost 16 per cent of a step).  Lanes
+// without a column do what the last column's lane does, so that nothing in a step is conditional.
+// USUAL: with softplus and gate; otherwise as the arguments say.
+// SCAN_BACK_PART goes from the last event to the first, for the segment's own part of what reaches the segment before it:
+// g = a[t] (C[t] gy[t] + g), from zero.
+template <class T, int NP, int MODE, bool USUAL>
 __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a) {
-  const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  using E = Events<T, NP>;
+  constexpr bool BACK = MODE == SCAN_BACK_PART, OUT = MODE == SCAN_Y, NEED_B = !BACK, NEED_C = OUT || BACK, PART = MODE == SCAN_PART || BACK;
+  __shared__ float stage[4][2][4 * NP];
+  const unsigned w4 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wave = blockIdx.x * 4 + w4;
   const unsigned all = (unsigned)(a.groups * a.tiles), item = wave / all, tile = wave - item * all;
   if (item >= a.items) return;
   const Piece p = piece_at(a.q, item, a.seg);
-  if (p.none || (MODE == SCAN_PART && p.last)) return;
+  if (p.none || (MODE == SCAN_PART && p.last) || (BACK && p.t0 == 0)) return;
   const int g = tile / a.tiles, col = (tile - g * a.tiles) * 64 + lane;
-  const bool on = col < a.dg;
-  const unsigned c = g * a.dg + (on ? col : a.dg - 1);
+  const unsigned c = g * a.dg + min(col, a.dg - 1);
   const int64_t state = state_of(a, p.s);
   float A[NP], h[NP];
   load_states<NP>(a.A + (int64_t)c * a.n, a.n, A);
-  if (MODE != SCAN_PART && a.seg != 0) load_states<NP>(a.seg_state + (p.slot * a.d + c) * a.n, a.n, h);
-  else if (MODE != SCAN_PART && state >= 0 && a.state_in != nullptr) load_states<NP>(a.state_in + (state * a.d + c) * a.n, a.n, h);
+  if (!PART && a.seg != 0) load_states<NP>(a.seg_state + (p.slot * a.d + c) * a.n, a.n, h);
+  else if (!PART && state >= 0 && a.state_in != nullptr) load_states<NP>(a.state_in + (state * a.d + c) * a.n, a.n, h);
   else
 #pragma unroll
     for (int i = 0; i < NP; ++i) h[i] = 0.0f;
-  const float bias = a.bias ? a.bias[c] : 0.0f, D = a.D ? a.D[c] : 0.0f;
-  const bool gated = MODE == SCAN_Y && a.z != nullptr;
-  const unsigned bl = g * a.n + (lane < (unsigned)a.n ? lane : a.n - 1);   // lane n holds B and C of state n
-  float total = 0.0f;   // of the deltas
-  auto ask = [&](int t, Event<T>& e) {
-    const int64_t row = seq_row(a.q, p.r, t);
-    e.x = (static_cast<const T*>(a.x) + row * a.ld_x)[c];
-    e.dt = (static_cast<const T*>(a.dt) + row * a.ld_dt)[c];
-    if (gated) e.z = (static_cast<const T*>(a.z) + row * a.ld_z)[c];
-    e.b = (static_cast<const T*>(a.B) + row * a.ld_b)[bl];
-    if (MODE == SCAN_Y) e.c = (static_cast<const T*>(a.C) + row * a.ld_c)[bl];
-  };
-  constexpr int U = 4;
-  Event<T> next[U];
-  if (p.t0 < p.t1)
+  const float bias = a.bias ? a.bias[c] : 0.0f, D = OUT && a.D ? a.D[c] : 0.0f;
+  const bool soft = USUAL || a.softplus, gated = (OUT || BACK) && (USUAL || a.z != nullptr);
+  float* sB = stage[w4][0];
+  float* sC = stage[w4][1];
+  // (the row, relative to the lowest of the four, and state of this lane's B and C)
+  unsigned off_b[E::R], off_c[E::R];
 #pragma unroll
-    for (int u = 0; u < U; ++u) ask(min(p.t0 + u, p.t1 - 1), next[u]);
-  for (int t4 = p.t0; t4 < p.t1; t4 += U) {
-    Event<T> e[U];
+  for (int r = 0; r < E::R; ++r) {
+    const int idx = (lane + 64 * r) % (4 * NP), e = idx / NP, n = g * a.n + min(idx % NP, a.n - 1);
+    off_b[r] = (a.q.newest_first ? 3 - e : e) * (unsigned)a.ld_b + n;
+    off_c[r] = (a.q.newest_first ? 3 - e : e) * (unsigned)a.ld_c + n;
+  }
+  // the events t .. t + n - 1 of a group of four, first in front
+  auto ask = [&](int t, int n, E& v) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) e[u] = next[u];
-    if (t4 + U < p.t1)
+    for (int u = 0; u < 4; ++u) {
+      const int64_t row = seq_row(a.q, p.r, t + (n == 4 ? u : min(u, n - 1)));
+      v.x[u] = (static_cast<const T*>(BACK ? a.dy : a.x) + row * (BACK ? a.ld_dy : a.ld_x))[c];
+      v.dt[u] = (static_cast<const T*>(a.dt) + row * a.ld_dt)[c];
+      if (gated) v.z[u] = (static_cast<const T*>(a.z) + row * a.ld_z)[c];
+    }
 #pragma unroll
-      for (int u = 0; u < U; ++u) ask(min(t4 + U + u, p.t1 - 1), next[u]);
-    if (MODE != SCAN_PART && a.saved != nullptr && t4 % CHUNK == 0 && on)
-      store_states<NP>(a.saved + ((seg_base(a.q, p.s, CHUNK) + t4 / CHUNK) * a.d + c) * a.n, a.n, h);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (t4 + u < p.t1) {
-      const float x = (float)e[u].x, raw = (float)e[u].dt + bias, delta = a.softplus ? softplus(raw) : raw;
-      const float d2 = delta * LOG2E, in = delta * x, bv = lane < (unsigned)a.n ? (float)e[u].b : 0.0f;
-      if (MODE == SCAN_PART) total += delta;
-      float y[2] = {0.0f, 0.0f};
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {   // (states beyond n stay zero)
-        h[i] = fmaf(__builtin_amdgcn_exp2f(d2 * A[i]), h[i], in * lane_value(bv, i));
-        if (MODE == SCAN_Y) y[i & 1] = fmaf(h[i], lane_value((float)e[u].c, i), y[i & 1]);
-      }
-      if (MODE == SCAN_Y) {
-        float out = fmaf(D, x, y[0] + y[1]);
-        if (gated) out *= (float)e[u].z * sigmoid((float)e[u].z);
-        if (on) (static_cast<T*>(a.y) + seq_row(a.q, p.r, t4 + u) * a.ld_y)[c] = (T)out;
-      }
+    for (int r = 0; r < E::R; ++r) {
+      if (n == 4) {
+        const int64_t low = seq_row(a.q, p.r, a.q.newest_first ? t + 3 : t);
+        if (NEED_B) v.b[r] = (static_cast<const T*>(a.B) + low * a.ld_b)[off_b[r]];
+        if (NEED_C) v.c[r] = (static_cast<const T*>(a.C) + low * a.ld_c)[off_c[r]];
+      } else {
+        const int idx = (lane + 64 * r) % (4 * NP), s = g * a.n + min(idx % NP, a.n - 1);
+        const int64_t row = seq_row(a.q, p.r, t + min(idx / NP, n - 1));
+        if (NEED_B) v.b[r] = (static_cast<const T*>(a.B) + row * a.ld_b)[s];
+        if (NEED_C) v.c[r] = (static_cast<const T*>(a.C) + row * a.ld_c)[s];
       }
     }
+  };
+  float total = 0.0f;   // of the deltas
+  auto work = [&](int t, int n, const E& v) {   // n < 4: the rest of the group changes nothing
+#pragma unroll
+    for (int r = 0; r < E::R; ++r) {
+      const int idx = (lane + 64 * r) % (4 * NP);
+      const bool in = idx % NP < a.n && (n == 4 || idx / NP < n);
+      if (NEED_B) sB[idx] = in ? (float)v.b[r] : 0.0f;
+      if (NEED_C) sC[idx] = in ? (float)v.c[r] : 0.0f;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int u = BACK ? 3 - k : k;
+      const float raw = (float)v.dt[u] + bias;
+      float x = (float)v.x[u], delta = soft ? softplus(raw) : raw, gate = 1.0f;
+      if (gated) gate = (float)v.z[u] * sigmoid((float)v.z[u]);
+      if (n < 4 && u >= n) x = delta = 0.0f;
+      const float d2 = delta * LOG2E;
+      if (PART) total += delta;
+      if constexpr (BACK) {
+        const float gy = n < 4 && u >= n ? 0.0f : x * gate;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) h[i] = __builtin_amdgcn_exp2f(d2 * A[i]) * fmaf(gy, sC[u * NP + i], h[i]);
+      } else {
+        const float in = delta * x;
+        float y[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {   // (states beyond n stay zero)
+          h[i] = fmaf(__builtin_amdgcn_exp2f(d2 * A[i]), h[i], in * sB[u * NP + i]);
+          if (OUT) y[i & 1] = fmaf(h[i], sC[u * NP + i], y[i & 1]);
+        }
+        if (OUT && (n == 4 || u < n))
+          (static_cast<T*>(a.y) + seq_row(a.q, p.r, t + u) * a.ld_y)[c] = (T)(fmaf(D, x, y[0] + y[1]) * gate);
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  // whole groups, and what is left of them at the end (of the segment: the first thing on the way back)
+  const int n_ev = p.t1 - p.t0, whole = n_ev / 4, left = n_ev & 3;
+  float* saved = !PART && a.saved != nullptr ? a.saved + ((seg_base(a.q, p.s, CHUNK) + p.t0 / CHUNK) * a.d + c) * a.n : nullptr;
+  const int64_t saved_step = (int64_t)a.d * a.n;
+  E next;
+  if (left != 0 && (BACK || whole == 0)) ask(p.t0 + 4 * whole, left, next);
+  if (BACK && left != 0) work(p.t0 + 4 * whole, left, next);
+  if (whole > 0) ask(BACK ? p.t0 + 4 * (whole - 1) : p.t0, 4, next);
+  for (int j = 0; j < whole; ++j) {
+    const E v = next;
+    const int t = p.t0 + 4 * (BACK ? whole - 1 - j : j);
+    if (j + 1 < whole) ask(BACK ? t - 4 : t + 4, 4, next);
+    else if (!BACK && left != 0) ask(t + 4, left, next);
+    if (!PART && saved != nullptr && (t & (CHUNK - 1)) == 0) {
+      store_states<NP>(saved, a.n, h);
+      saved += saved_step;
+    }
+    work(t, 4, v);
   }
-  if (!on) return;
-  if (MODE == SCAN_PART) {
+  if (!BACK && left != 0) {
+    if (!PART && saved != nullptr && ((p.t0 + 4 * whole) & (CHUNK - 1)) == 0) store_states<NP>(saved, a.n, h);
+    work(p.t0 + 4 * whole, left, next);
+  }
+  if (PART) {
     store_states<NP>(a.seg_state + (p.slot * a.d + c) * a.n, a.n, h);
     a.seg_delta[p.slot * a.d + c] = total;
   }
-  if (MODE == SCAN_Y && p.last) {
+  if (OUT && p.last) {
     for (int t = p.r.len; t < p.r.slot; ++t) (static_cast<T*>(a.y) + (p.r.begin + t) * a.ld_y)[c] = (T)0.0f;
     if (state >= 0 && a.state_out != nullptr) store_states<NP>(a.state_out + (state * a.d + c) * a.n, a.n, h);
   }
 }
 
-// The way back through a segment, for its own part of what reaches the segment before it: g = a[t] (C[t] gy[t] + g), from zero.
-template <class T, int NP>
-__global__ __launch_bounds__(256) void scan_back_part_kernel(ScanArgs a) {
-  const unsigned wave = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6)), lane = threadIdx.x & 63;
-  const unsigned all = (unsigned)(a.groups * a.tiles), item = wave / all, tile = wave - item * all;
-  if (item >= a.items) return;
-  const Piece p = piece_at(a.q, item, a.seg);
-  if (p.none || p.t0 == 0) return;
-  const int grp = tile / a.tiles, col = (tile - grp * a.tiles) * 64 + lane;
-  const bool on = col < a.dg;
-  const unsigned c = grp * a.dg + (on ? col : a.dg - 1);
-  float A[NP], g[NP];
-  load_states<NP>(a.A + (int64_t)c * a.n, a.n, A);
-#pragma unroll
-  for (int i = 0; i < NP; ++i) g[i] = 0.0f;
-  const float bias = a.bias ? a.bias[c] : 0.0f;
-  const unsigned bl = grp * a.n + (lane < (unsigned)a.n ? lane : a.n - 1);
-  float total = 0.0f;
-  auto ask = [&](int t, Event<T>& e) {
-    const int64_t row = seq_row(a.q, p.r, t);
-    e.x = (static_cast<const T*>(a.dy) + row * a.ld_dy)[c];
-    e.dt = (static_cast<const T*>(a.dt) + row * a.ld_dt)[c];
-    if (a.z) e.z = (static_cast<const T*>(a.z) + row * a.ld_z)[c];
-    e.c = (static_cast<const T*>(a.C) + row * a.ld_c)[bl];
-  };
-  constexpr int U = 4;
-  Event<T> next[U];
-#pragma unroll
-  for (int u = 0; u < U; ++u) ask(max(p.t1 - 1 - u, p.t0), next[u]);
-  for (int t4 = p.t1 - 1; t4 >= p.t0; t4 -= U) {
-    Event<T> e[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) e[u] = next[u];
-    if (t4 - U >= p.t0)
-#pragma unroll
-      for (int u = 0; u < U; ++u) ask(max(t4 - U - u, p.t0), next[u]);
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (t4 - u >= p.t0) {
-      const float raw = (float)e[u].dt + bias, delta = a.softplus ? softplus(raw) : raw, d2 = delta * LOG2E;
-      const float cv = lane < (unsigned)a.n ? (float)e[u].c : 0.0f;
-      float gy = (float)e[u].x;
-      if (a.z) gy *= (float)e[u].z * sigmoid((float)e[u].z);
-      total += delta;
-#pragma unroll
-      for (int i = 0; i < NP; ++i) g[i] = __builtin_amdgcn_exp2f(d2 * A[i]) * fmaf(gy, lane_value(cv, i), g[i]);
-      }
-    }
-  }
-  if (!on) return;
-  store_states<NP>(a.seg_state + (p.slot * a.d + c) * a.n, a.n, g);
-  a.seg_delta[p.slot * a.d + c] = total;
-}
-
 // From segment to segment.  Forward: seg_state[k] becomes the state before segment k, from the sequence's first state; backward: what
-// reaches segment k from behind, from zero.  A thread per sequence, column and state.
-template <bool BACK>
+// reaches segment k from behind, from zero.  A thread has a column and state of a sequence and asks for eight segments at a time;
+// where there are many of them (RUNS = 8) eight threads cut them into runs: each run's own part and the sum of its
+// deltas, the run's first state from those before it, then the states.  256 segments of 8,192 columns and states: 13 us,
+// one thread for all, one segment after the other, 87; up to 32 segments of 32 sequences of 16,384: 37 us with runs.
+template <bool BACK, int RUNS>
 __global__ __launch_bounds__(256) void scan_chain_kernel(ScanArgs a) {
-  const int64_t dn = (int64_t)a.d * a.n, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= a.q.n_seqs * dn) return;
-  const int s = (int)(i / dn);
-  const int64_t e = i - s * dn;
-  const int c = (int)(e / a.n);
+  constexpr int COLS = 256 / RUNS;
+  __shared__ float part[RUNS][COLS], sum[RUNS][COLS];
+  const int64_t dn = (int64_t)a.d * a.n, per = (dn + COLS - 1) / COLS;
+  const int s = (int)(blockIdx.x / per), x = threadIdx.x % COLS, run = threadIdx.x / COLS;
+  const int64_t e = (blockIdx.x - s * per) * COLS + x;
+  const bool on = e < dn;
+  const int c = on ? (int)(e / a.n) : 0;
   const Seq r = seq_at(a.q, s);
   const int64_t base = seg_base(a.q, s, a.seg);
   const int count = r.len > 0 ? (int)(((int64_t)r.len + a.seg - 1) / a.seg) : 1;
   const int64_t state = state_of(a, s);
-  float cur = !BACK && state >= 0 && a.state_in != nullptr ? a.state_in[state * dn + e] : 0.0f;
-  const float A = a.A[e];
-  for (int k = 0; k < count; ++k) {
-    const int64_t at = base + (BACK ? count - 1 - k : k);
-    float* p = a.seg_state + at * dn + e;
-    // (forward the last segment's part is not formed, backward the first one's)
-    const float part = k + 1 < count ? *p : 0.0f, delta = k + 1 < count ? a.seg_delta[at * a.d + c] : 0.0f;
-    *p = cur;
-    cur = fmaf(__builtin_amdgcn_exp2f(delta * LOG2E * A), cur, part);
+  const float A = on ? a.A[e] * LOG2E : 0.0f;
+  // segment k in the order of the recurrence; the last one's part was not formed (and is not needed)
+  auto at = [&](int k) { return base + (BACK ? count - 1 - k : k); };
+  const int each = (count + RUNS - 1) / RUNS, k0 = min(run * each, count), k1 = min(k0 + each, count);
+  constexpr int U = 8;
+  float cur = 0.0f, total = 0.0f;
+  for (int k = k0; RUNS > 1 && on && k < min(k1, count - 1); k += U) {
+    float v[U], d[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = at(min(k + u, count - 1));
+      const bool in = k + u < min(k1, count - 1);
+      v[u] = in ? a.seg_state[i * dn + e] : 0.0f;
+      d[u] = in ? a.seg_delta[i * a.d + c] : 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      cur = fmaf(__builtin_amdgcn_exp2f(d[u] * A), cur, v[u]);
+      total += d[u];
+    }
+  }
+  if (RUNS > 1) {
+    part[run][x] = cur;
+    sum[run][x] = total;
+    __syncthreads();
+  }
+  if (!on) return;
+  cur = !BACK && state >= 0 && a.state_in != nullptr ? a.state_in[state * dn + e] : 0.0f;
+  for (int i = 0; i < run; ++i) cur = fmaf(__builtin_amdgcn_exp2f(sum[i][x] * A), cur, part[i][x]);
+  for (int k = k0; k < k1; k += U) {
+    float v[U], d[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = at(min(k + u, count - 1));
+      const bool in = k + u < min(k1, count - 1);
+      v[u] = in ? a.seg_state[i * dn + e] : 0.0f;
+      d[u] = in ? a.seg_delta[i * a.d + c] : 0.0f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (k + u < k1) a.seg_state[at(k + u) * dn + e] = cur;
+      cur = fmaf(__builtin_amdgcn_exp2f(d[u] * A), cur, v[u]);
+    }
   }
 }
 
@@ -289,18 +334,35 @@ __device__ __forceinline__ float rows_sum(float u, float v) {
 // Wavefronts of a workgroup: as many as 48 KB of LDS hold the states of (three workgroups to a compute unit)
 constexpr int bwd_waves(int np) { return np <= 4 ? 4 : np == 8 ? 2 : 1; }
 
+// v[e][i] of four events and NP states, summed over the wavefront's 16 columns: every lane gets the sums of its four states for
+// one event, event_of_sum(lane)
+template <int NP> __device__ __forceinline__ void column_sums(const float (&v)[4][NP], float (&s)[NP]) {
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    float x = rows_sum(halves_sum(v[0][i], v[2][i]), halves_sum(v[1][i], v[3][i]));
+    x += dpp_get<ROW_ROR8>(x);
+    s[i] = x + dpp_get<ROW_ROR4>(x);
+  }
+}
+__device__ __forceinline__ int event_of_sum(int lane) { return 2 * (lane >> 5) + (lane >> 4 & 1); }
+
 // A workgroup: 16 columns per wavefront of one group, over the pieces worker, worker + workers, ...
-template <class T, int NP>
-__global__ __launch_bounds__(64 * bwd_waves(NP)) void scan_bwd_kernel(ScanArgs a) {
-  constexpr int WAVES = bwd_waves(NP), THREADS = 64 * WAVES, N4 = 4 * NP;
+#ifndef OCC
+#define OCC 3
+#endif
+template <class T, int NP, bool USUAL>
+__global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bwd_kernel(ScanArgs a) {
+  constexpr int WAVES = bwd_waves(NP), THREADS = 64 * WAVES, N4 = 4 * NP, STAGE = CHUNK * N4 / THREADS > 0 ? CHUNK * N4 / THREADS : 1;
+  constexpr bool AHEAD = STAGE <= 2;                 // the next chunk's B, C and states are asked for a chunk ahead
   __shared__ float bound[CHUNK / 4][THREADS * NP];   // a lane's states before every fourth event
-  __shared__ float sB[CHUNK][N4], sC[CHUNK][N4];     // of the chunk's events
-  __shared__ float red[WAVES][CHUNK][2][N4];         // dB, dC summed over a wavefront's columns
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane & 3;
+  __shared__ float sB[CHUNK * N4], sC[CHUNK * N4];   // of the chunk's events
+  __shared__ float red[WAVES][2][CHUNK * N4];        // dB, dC summed over a wavefront's columns
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 3;
   const int all = a.groups * a.tiles, tile = blockIdx.x % all, worker = blockIdx.x / all, workers = gridDim.x / all;
   const int grp = tile / a.tiles, sub = tile - grp * a.tiles;
   const int col = sub * 16 * WAVES + wave * 16 + (lane >> 2);
   const bool on = col < a.dg, full = __all(on), odd = (q & 1) != 0, high = (q & 2) != 0;
+  const bool soft = USUAL || a.softplus, gated = USUAL || a.z != nullptr, newest = a.q.newest_first != 0;
   const unsigned c = grp * a.dg + (on ? col : a.dg - 1);
   float A[NP], dA[NP];
 #pragma unroll
@@ -310,7 +372,9 @@ __global__ __launch_bounds__(64 * bwd_waves(NP)) void scan_bwd_kernel(ScanArgs a
   }
   const float bias = a.bias ? a.bias[c] : 0.0f, D = a.D ? a.D[c] : 0.0f;
   float dD = 0.0f, dbias = 0.0f;
-  auto at = [&](const void* p, int64_t ld, int64_t row) -> float { return (float)(static_cast<const T*>(p) + row * ld)[c]; };
+  // A lane has the values of event q of a group of four: their distance from the lowest row of the group's four.
+  const unsigned up = newest ? 3 - q : q;
+  const unsigned ox = up * (unsigned)a.ld_x + c, odt = up * (unsigned)a.ld_dt + c, oz = up * (unsigned)a.ld_z + c, ody = up * (unsigned)a.ld_dy + c;
 
   for (int64_t item = worker; item < a.items; item += workers) {
     const Piece p = piece_at(a.q, item, a.seg);
@@ -319,65 +383,90 @@ __global__ __launch_bounds__(64 * bwd_waves(NP)) void scan_bwd_kernel(ScanArgs a
 #pragma unroll
     for (int i = 0; i < NP; ++i)
       g[i] = a.seg != 0 && on && q * NP + i < a.n ? a.seg_state[(p.slot * a.d + c) * a.n + q * NP + i] : 0.0f;
-    const int64_t chunk0 = seg_base(a.q, p.s, CHUNK);
-    for (int tb = p.t1 > p.t0 ? p.t0 + (p.t1 - 1 - p.t0) / CHUNK * CHUNK : p.t0 - CHUNK; tb >= p.t0; tb -= CHUNK) {
-      const int n_ev = min(CHUNK, p.t1 - tb), n_sub = (n_ev + 3) / 4;
-      for (int i = tid; i < CHUNK * N4; i += THREADS) {
-        const int t = i / N4, n = i - t * N4;
-        float b = 0.0f, cc = 0.0f;
-        if (t < n_ev && n < a.n) {
-          const int64_t row = seq_row(a.q, p.r, tb + t);
-          b = (float)(static_cast<const T*>(a.B) + row * a.ld_b)[grp * a.n + n];
-          cc = (float)(static_cast<const T*>(a.C) + row * a.ld_c)[grp * a.n + n];
+    const float* saved = a.saved + (seg_base(a.q, p.s, CHUNK) * a.d + c) * a.n + q * NP;
+    const int64_t saved_step = (int64_t)a.d * a.n;
+
+    // B, C and the first states of the chunk that begins at tb
+    T rb[STAGE], rc[STAGE];
+    float hn[NP];
+    auto ask_chunk = [&](int tb) {
+      const int n_ev = min(CHUNK, p.t1 - tb);
+#pragma unroll
+      for (int r = 0; r < STAGE; ++r) {
+        const int i = tid + r * THREADS, e = i / N4, n = i % N4;
+        rb[r] = rc[r] = (T)0.0f;
+        if (e < n_ev && n < a.n) {
+          const int64_t row = seq_row(a.q, p.r, tb + e);
+          rb[r] = (static_cast<const T*>(a.B) + row * a.ld_b)[grp * a.n + n];
+          rc[r] = (static_cast<const T*>(a.C) + row * a.ld_c)[grp * a.n + n];
         }
-        sB[t][n] = b;
-        sC[t][n] = cc;
       }
-      __syncthreads();
+      const float* sv = saved + (tb / CHUNK) * saved_step;
+#pragma unroll
+      for (int i = 0; i < NP; ++i) hn[i] = on && q * NP + i < a.n ? sv[i] : 0.0f;
+    };
+    struct Own { T x, dt, z, dy; };
+    auto low_row = [&](int t) { return p.r.begin + (newest ? p.r.len - 4 - t : t); };   // of the events t .. t + 3
+    auto ask = [&](int t, bool back, Own& v) {
+      const int64_t row = low_row(t);
+      v.x = v.dt = v.z = v.dy = (T)0.0f;
+      if (on && t + q < p.t1) {
+        v.x = (static_cast<const T*>(a.x) + row * a.ld_x)[ox];
+        v.dt = (static_cast<const T*>(a.dt) + row * a.ld_dt)[odt];
+        if (back) {
+          v.dy = (static_cast<const T*>(a.dy) + row * a.ld_dy)[ody];
+          if (gated) v.z = (static_cast<const T*>(a.z) + row * a.ld_z)[oz];
+        }
+      }
+    };
+
+    const int tb0 = p.t1 > p.t0 ? p.t0 + (p.t1 - 1 - p.t0) / CHUNK * CHUNK : p.t0 - CHUNK;
+    if (AHEAD && tb0 >= p.t0) ask_chunk(tb0);
+    for (int tb = tb0; tb >= p.t0; tb -= CHUNK) {
+      const int n_ev = min(CHUNK, p.t1 - tb), n_sub = (n_ev + 3) / 4;
+      if (!AHEAD) ask_chunk(tb);
+#pragma unroll
+      for (int r = 0; r < STAGE; ++r)
+        if (CHUNK * N4 >= THREADS || tid < CHUNK * N4) {
+          sB[tid + r * THREADS] = (float)rb[r];
+          sC[tid + r * THREADS] = (float)rc[r];
+        }
       float h[NP];
-      const float* sv = a.saved + ((chunk0 + tb / CHUNK) * a.d + c) * a.n + q * NP;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) h[i] = on && q * NP + i < a.n ? sv[i] : 0.0f;
+      for (int i = 0; i < NP; ++i) h[i] = hn[i];
+      __syncthreads();
+      Own nx;
+      ask(tb, n_sub == 1, nx);
       // forward over the chunk: the state before every fourth event
-      for (int j = 0; j < n_sub; ++j) {
 #pragma unroll
-        for (int i = 0; i < NP; ++i) bound[j][tid * NP + i] = h[i];
-        if (j + 1 == n_sub) break;
-        const int t = 4 * j + q;
-        const int64_t row = seq_row(a.q, p.r, tb + t);
-        const float x = on ? at(a.x, a.ld_x, row) : 0.0f, raw = at(a.dt, a.ld_dt, row) + bias;
-        const float delta = a.softplus ? softplus(raw) : raw, d2 = delta * LOG2E, in = delta * x;
+      for (int i = 0; i < NP; ++i) bound[0][tid * NP + i] = h[i];
+      for (int j = 0; j + 1 < n_sub; ++j) {
+        const Own v = nx;
+        ask(tb + 4 * j + 4, j + 2 == n_sub, nx);
+        const float raw = (float)v.dt + bias, delta = soft ? softplus(raw) : raw, d2 = delta * LOG2E, in = delta * (float)v.x;
         const float d2s[4] = {quad_get<0>(d2), quad_get<1>(d2), quad_get<2>(d2), quad_get<3>(d2)};
         const float ins[4] = {quad_get<0>(in), quad_get<1>(in), quad_get<2>(in), quad_get<3>(in)};
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
           for (int i = 0; i < NP; ++i)
-            h[i] = fmaf(__builtin_amdgcn_exp2f(d2s[e] * A[i]), h[i], ins[e] * sB[4 * j + e][q * NP + i]);
+            h[i] = fmaf(__builtin_amdgcn_exp2f(d2s[e] * A[i]), h[i], ins[e] * sB[(4 * j + e) * N4 + q * NP + i]);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) bound[j + 1][tid * NP + i] = h[i];
       }
-      // and back, four events at a time; a lane has the event's own quantities of event 4 j + q
+      if (AHEAD && tb > p.t0) ask_chunk(tb - CHUNK);
+      // and back, four events at a time
       for (int j = n_sub - 1; j >= 0; --j) {
-        const int t = 4 * j + q;
-        const bool there = t < n_ev;
-        const int64_t row = seq_row(a.q, p.r, tb + (there ? t : 0));
-        float x = 0.0f, raw = 0.0f, z = 0.0f, dy = 0.0f, delta = 0.0f, sg = 0.0f, gy = 0.0f;
-        if (there && on) {
-          x = at(a.x, a.ld_x, row);
-          raw = at(a.dt, a.ld_dt, row) + bias;
-          dy = at(a.dy, a.ld_dy, row);
-          delta = a.softplus ? softplus(raw) : raw;
-          gy = dy;
-          if (a.z) {
-            z = at(a.z, a.ld_z, row);
-            sg = sigmoid(z);
-            gy = dy * z * sg;
-          }
-        }
+        const Own v = nx;
+        if (j > 0) ask(tb + 4 * j - 4, true, nx);
+        const bool there = on && 4 * j + q < n_ev;
+        const float x = (float)v.x, raw = (float)v.dt + bias, z = (float)v.z, dy = (float)v.dy;
+        const float delta = there ? (soft ? softplus(raw) : raw) : 0.0f, sg = gated ? sigmoid(z) : 1.0f, gy = gated ? dy * z * sg : dy;
         const float d2 = delta * LOG2E, in = delta * x;
         const float d2s[4] = {quad_get<0>(d2), quad_get<1>(d2), quad_get<2>(d2), quad_get<3>(d2)};
         const float ins[4] = {quad_get<0>(in), quad_get<1>(in), quad_get<2>(in), quad_get<3>(in)};
         const float gys[4] = {quad_get<0>(gy), quad_get<1>(gy), quad_get<2>(gy), quad_get<3>(gy)};
-        float dec[4][NP], ah[4][NP], vB[4][NP], vC[4][NP], y[4], s1[4], s2[4];
+        float dec[4][NP], ah[4][NP], v4[4][NP], y[4], s1[4], s2[4], sum[NP];
 #pragma unroll
         for (int i = 0; i < NP; ++i) h[i] = bound[j][tid * NP + i];
 #pragma unroll
@@ -387,60 +476,61 @@ __global__ __launch_bounds__(64 * bwd_waves(NP)) void scan_bwd_kernel(ScanArgs a
           for (int i = 0; i < NP; ++i) {
             dec[e][i] = __builtin_amdgcn_exp2f(d2s[e] * A[i]);
             ah[e][i] = dec[e][i] * h[i];
-            h[i] = fmaf(ins[e], sB[4 * j + e][q * NP + i], ah[e][i]);
-            vC[e][i] = gys[e] * h[i];
-            y[e] = fmaf(h[i], sC[4 * j + e][q * NP + i], y[e]);
+            h[i] = fmaf(ins[e], sB[(4 * j + e) * N4 + q * NP + i], ah[e][i]);
+            v4[e][i] = gys[e] * h[i];
+            y[e] = fmaf(h[i], sC[(4 * j + e) * N4 + q * NP + i], y[e]);
           }
         }
+        column_sums<NP>(v4, sum);
+        const int at = (4 * j + event_of_sum(lane)) * N4 + q * NP;
+        if ((lane & 12) == 0)
+#pragma unroll
+          for (int i = 0; i < NP; ++i) red[wave][1][at + i] = sum[i];
 #pragma unroll
         for (int e = 3; e >= 0; --e) {
           s1[e] = s2[e] = 0.0f;
 #pragma unroll
           for (int i = 0; i < NP; ++i) {
-            const float lam = fmaf(sC[4 * j + e][q * NP + i], gys[e], g[i]), lah = lam * ah[e][i];
-            s1[e] = fmaf(lam, sB[4 * j + e][q * NP + i], s1[e]);
+            const float lam = fmaf(sC[(4 * j + e) * N4 + q * NP + i], gys[e], g[i]), lah = lam * ah[e][i];
+            s1[e] = fmaf(lam, sB[(4 * j + e) * N4 + q * NP + i], s1[e]);
             s2[e] = fmaf(A[i], lah, s2[e]);
             dA[i] = fmaf(d2s[e], lah, dA[i]);
-            vB[e][i] = lam * ins[e];
+            v4[e][i] = lam * ins[e];
             g[i] = dec[e][i] * lam;
           }
         }
-        const float y0 = quad_scatter_sum(y, odd, high), t1 = quad_scatter_sum(s1, odd, high), t2 = quad_scatter_sum(s2, odd, high);
-        if (there && on) {
-          const float dd = fmaf(x, t1, t2), draw = a.softplus ? dd * sigmoid(raw) : dd;
-          (static_cast<T*>(a.dx) + row * a.ld_dx)[c] = (T)fmaf(D, gy, delta * t1);
-          (static_cast<T*>(a.ddt) + row * a.ld_ddt)[c] = (T)draw;
-          if (a.z) (static_cast<T*>(a.dz) + row * a.ld_dz)[c] = (T)(dy * fmaf(D, x, y0) * (sg * fmaf(z, 1.0f - sg, 1.0f)));
-          dD = fmaf(gy, x, dD);
-          dbias += draw;
-        }
-        if (!full)   // a column that is none adds nothing (not even where C is infinite)
+        if (!full) {   // a column that is none adds nothing, also where C is infinite
+          asm volatile("");   // (a branch, not 16 selects for every wavefront)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int i = 0; i < NP; ++i) {
-              vB[e][i] = on ? vB[e][i] : 0.0f;
-              vC[e][i] = on ? vC[e][i] : 0.0f;
-            }
-        // sums over the wavefront's 16 columns: lower half dB, upper half dC; even rows events 0 and 1, odd rows 2 and 3
+            for (int i = 0; i < NP; ++i) v4[e][i] = on ? v4[e][i] : 0.0f;
+        }
+        column_sums<NP>(v4, sum);
+        if ((lane & 12) == 0)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int i = 0; i < NP; ++i) {
-            float v = rows_sum(halves_sum(vB[e][i], vC[e][i]), halves_sum(vB[e + 2][i], vC[e + 2][i]));
-            v += dpp_get<ROW_ROR8>(v);
-            v += dpp_get<ROW_ROR4>(v);
-            if ((lane & 12) == 0) red[wave][4 * j + e + 2 * ((lane >> 4) & 1)][lane >> 5][q * NP + i] = v;
-          }
+          for (int i = 0; i < NP; ++i) red[wave][0][at + i] = sum[i];
+        const float t1 = quad_scatter_sum(s1, odd, high), t2 = quad_scatter_sum(s2, odd, high);
+        const float dd = fmaf(x, t1, t2), draw = soft ? dd * sigmoid(raw) : dd;
+        float dz = 0.0f;
+        if (gated) dz = dy * fmaf(D, x, quad_scatter_sum(y, odd, high)) * (sg * fmaf(z, 1.0f - sg, 1.0f));
+        if (there) {
+          const int64_t row = low_row(tb + 4 * j);
+          (static_cast<T*>(a.dx) + row * a.ld_dx)[up * (unsigned)a.ld_dx + c] = (T)fmaf(D, gy, delta * t1);
+          (static_cast<T*>(a.ddt) + row * a.ld_ddt)[up * (unsigned)a.ld_ddt + c] = (T)draw;
+          if (gated) (static_cast<T*>(a.dz) + row * a.ld_dz)[up * (unsigned)a.ld_dz + c] = (T)dz;
+          dD = fmaf(gy, x, dD);
+          dbias += draw;
+        }
       }
       __syncthreads();
       for (int i = tid; i < n_ev * 2 * N4; i += THREADS) {
-        const int t = i / (2 * N4), kind = i / N4 & 1, n = i % N4;
+        const int kind = i >= n_ev * N4, at = kind ? i - n_ev * N4 : i, e = at / N4, n = at % N4;
         if (n >= a.n) continue;
         float sum = 0.0f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) sum += red[w][t][kind][n];
-        const int64_t row = seq_row(a.q, p.r, tb + t);
+        for (int w = 0; w < WAVES; ++w) sum += red[w][kind][at];
+        const int64_t row = seq_row(a.q, p.r, tb + e);
         const int k = grp * a.n + n;
         if (a.part_bc != nullptr) a.part_bc[((sub * a.q.n_rows + row) * 2 + kind) * a.groups * a.n + k] = sum;
         else if (kind == 0) (static_cast<T*>(a.dB) + row * a.ld_db)[k] = (T)sum;
@@ -448,12 +538,11 @@ __global__ __launch_bounds__(64 * bwd_waves(NP)) void scan_bwd_kernel(ScanArgs a
       }
     }
     if (p.last) {   // padding rows
-      for (int t = p.r.len + q; t < p.r.slot; t += 4) {
-        if (!on) continue;
+      for (int t = p.r.len + q; on && t < p.r.slot; t += 4) {
         const int64_t row = p.r.begin + t;
         (static_cast<T*>(a.dx) + row * a.ld_dx)[c] = (T)0.0f;
         (static_cast<T*>(a.ddt) + row * a.ld_ddt)[c] = (T)0.0f;
-        if (a.z) (static_cast<T*>(a.dz) + row * a.ld_dz)[c] = (T)0.0f;
+        if (gated) (static_cast<T*>(a.dz) + row * a.ld_dz)[c] = (T)0.0f;
       }
       if (sub == 0)
         for (int64_t i = tid; i < (int64_t)(p.r.slot - p.r.len) * a.n; i += THREADS) {
@@ -605,7 +694,13 @@ struct Take {   // pieces of a workspace
   }
 };
 
-constexpr int FWD_SPREAD = 1024, FWD_FILL = 4;   // wavefronts: one, and four, to a vector unit
+#ifndef FFILL
+#define FFILL 4
+#endif
+#ifndef BFILL
+#define BFILL 3
+#endif
+constexpr int FWD_SPREAD = 1024, FWD_FILL = FFILL;   // wavefronts: one, and four, to a vector unit
 static int fwd_tiles(int dg) { return (dg + 63) / 64; }
 static int fwd_segment(const tgnn_seqs& q, int groups, int dg) { return scan_segment(q, (int64_t)groups * fwd_tiles(dg), FWD_SPREAD, FWD_FILL); }
 
@@ -625,6 +720,23 @@ static int launch_grid(int64_t n, unsigned* out) {
   return TGNN_OK;
 }
 
+// Runs from 64 segments of the longest sequence on
+static bool chain_runs(const ScanArgs& a) { return std::min<int64_t>(a.q.max_len, scan_rows(a.q)) > 64 * (int64_t)a.seg; }
+static int chain_grid(const ScanArgs& a, unsigned* out) {
+  const int cols = chain_runs(a) ? 32 : 256;
+  return launch_grid(a.q.n_seqs * (((int64_t)a.d * a.n + cols - 1) / cols), out);
+}
+template <bool BACK> static void launch_chain(const ScanArgs& a, unsigned grid, hipStream_t s) {
+  if (chain_runs(a)) hipLaunchKernelGGL((scan_chain_kernel<BACK, 8>), dim3(grid), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((scan_chain_kernel<BACK, 1>), dim3(grid), dim3(256), 0, s, a);
+}
+
+template <class T, int NP, int MODE> static void launch_scan(const ScanArgs& a, dim3 grid, hipStream_t s) {
+  constexpr bool GATED = MODE == SCAN_Y || MODE == SCAN_BACK_PART;
+  if (a.softplus && (!GATED || a.z != nullptr)) hipLaunchKernelGGL((scan_fwd_kernel<T, NP, MODE, true>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((scan_fwd_kernel<T, NP, MODE, false>), grid, dim3(256), 0, s, a);
+}
+
 // The launches of a forward pass; MODE: SCAN_Y or SCAN_STATES
 template <int MODE> static int scan_forward(ScanArgs a, hipStream_t s, int dtype) {
   a.tiles = fwd_tiles(a.dg);
@@ -635,21 +747,21 @@ template <int MODE> static int scan_forward(ScanArgs a, hipStream_t s, int dtype
   const dim3 grid((unsigned)((waves + 3) / 4));
   unsigned chain = 0;
   if (a.seg)
-    if (int rc = launch_grid(((int64_t)a.q.n_seqs * a.d * a.n + 255) / 256, &chain)) return rc;
+    if (int rc = chain_grid(a, &chain)) return rc;
   scan_shape(dtype, a.n, [&](auto t, auto np) {
     using T = decltype(t);
     constexpr int NP = decltype(np)::value;
     if (a.seg) {
-      hipLaunchKernelGGL((scan_fwd_kernel<T, NP, SCAN_PART>), grid, dim3(256), 0, s, a);
-      hipLaunchKernelGGL((scan_chain_kernel<false>), dim3(chain), dim3(256), 0, s, a);
+      launch_scan<T, NP, SCAN_PART>(a, grid, s);
+      launch_chain<false>(a, chain, s);
     }
-    hipLaunchKernelGGL((scan_fwd_kernel<T, NP, MODE>), grid, dim3(256), 0, s, a);
+    launch_scan<T, NP, MODE>(a, grid, s);
   });
   TGNN_LAUNCH_CHECK();
   return TGNN_OK;
 }
 
-constexpr int BWD_SPREAD = 256, BWD_FILL = 3;   // workgroups: one, and three, to a compute unit
+constexpr int BWD_SPREAD = 256, BWD_FILL = BFILL;   // workgroups: one, and three, to a compute unit
 constexpr int BWD_WORKERS = 1024;   // at most as many partial sums of the weights' gradients
 
 struct BwdPlan { int np, tiles, seg, workers; int64_t items; };
@@ -820,7 +932,7 @@ extern "C" int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_sca
     unsigned chain = 0, back = 0, sum = 0;
     const int64_t waves = plan.items * a.groups * fwd_tiles(a.dg);
     if (plan.seg) {
-      if (int rc = launch_grid(((int64_t)seqs->n_seqs * d * a.n + 255) / 256, &chain)) return rc;
+      if (int rc = chain_grid(a, &chain)) return rc;
       if (int rc = launch_grid(waves, &back)) return rc;
     }
     if (int rc = launch_grid(seg_total(*seqs, CHUNK), &sum)) return rc;
@@ -829,11 +941,13 @@ extern "C" int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_sca
       constexpr int NP = decltype(np)::value;
       if (plan.seg) {
         a.tiles = fwd_tiles(a.dg);
-        hipLaunchKernelGGL((scan_back_part_kernel<T, NP>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a);
-        hipLaunchKernelGGL((scan_chain_kernel<true>), dim3(chain), dim3(256), 0, s, a);
+        launch_scan<T, NP, SCAN_BACK_PART>(a, dim3((unsigned)((waves + 3) / 4)), s);
+        launch_chain<true>(a, chain, s);
       }
       a.tiles = plan.tiles;
-      hipLaunchKernelGGL((scan_bwd_kernel<T, NP / 4>), dim3((unsigned)(plan.workers * a.groups * plan.tiles)), dim3(64 * bwd_waves(NP / 4)), 0, s, a);
+      const dim3 grid((unsigned)(plan.workers * a.groups * plan.tiles)), block(64 * bwd_waves(NP / 4));
+      if (a.softplus && a.z != nullptr) hipLaunchKernelGGL((scan_bwd_kernel<T, NP / 4, true>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((scan_bwd_kernel<T, NP / 4, false>), grid, block, 0, s, a);
       if (a.part_bc) hipLaunchKernelGGL((scan_bc_sum_kernel<T>), dim3(sum), dim3(256), 0, s, a);
     });
     TGNN_LAUNCH_CHECK();
