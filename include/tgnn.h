@@ -388,7 +388,7 @@ int32_t tgnn_profile_read(tgnn_ctx* ctx, int32_t stage, int32_t* out_count, doub
 typedef struct {
   const int64_t* indptr; /* [n_seqs + 1] or NULL */
   const int32_t* cnt;    /* [n_seqs] or NULL */
-  int64_t n_rows;        /* rows of every row array; n_rows < 2^34 */
+  int64_t n_rows;        /* rows of every row array; n_rows < 2^33 and n_rows / 8 + n_seqs < 2^31 */
   int32_t n_seqs, max_len, newest_first;
 } tgnn_seqs;
 

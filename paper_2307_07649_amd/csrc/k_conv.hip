@@ -15,8 +15,8 @@
 
 namespace tgnn {
 
-constexpr int CONV_SEG = 64;      // rows of a segment: 5 to 10 per cent of them are read twice with four taps
-constexpr int CONV_GRID = 1024;   // workgroups of the backward pass (partial rows of dw and db)
+constexpr int CONV_GRID = 768;    // workgroups of the backward pass (partial rows of dw and db): three to a compute unit
+constexpr int AHEAD = 4;          // rows on their way
 constexpr int CONV_ANY = TGNN_MAX_CONV_WIDTH;
 
 struct ConvArgs {
@@ -29,21 +29,36 @@ struct ConvArgs {
   void* y;                        // y, or dx
   float* part;                    // [grid, d W + d]
   int64_t ld_x, ld_dy, ld_y, items;
-  int d, width, n_states, silu, per_x;   // per_x: threads of a workgroup along the columns
+  int d, width, n_states, silu, per_x, bits;   // per_x: threads of a workgroup along the columns; segments of 2^bits rows
 };
 
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
 
-// taps of V columns; W == CONV_ANY: any number of them up to that, in the places behind
+// Taps of V columns; W == CONV_ANY: any number of them up to that, in the places behind.  (V * W values next to each other: as
+// vector loads, for which four bytes are aligned enough.)
 template <int V, int W> __device__ __forceinline__ void conv_taps(const ConvArgs& a, int c, float (&w)[W][V], float (&b)[V]) {
+  if constexpr (W != CONV_ANY) {
+    const FloatRun<V * W> r = *reinterpret_cast<const FloatRun<V * W>*>(a.w + (int64_t)c * W);
 #pragma unroll
-  for (int i = 0; i < V; ++i) {
+    for (int i = 0; i < V; ++i)
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-      const int k = j - (W - a.width);
-      w[j][i] = k >= 0 ? a.w[(int64_t)(c + i) * a.width + k] : 0.0f;
-    }
-    b[i] = a.bias ? a.bias[c + i] : 0.0f;
+      for (int j = 0; j < W; ++j) w[j][i] = r.v[i * W + j];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const int k = j - (W - a.width);
+        w[j][i] = k >= 0 ? a.w[(int64_t)(c + i) * a.width + k] : 0.0f;
+      }
+  }
+  if (a.bias) {
+    const FloatRun<V> r = *reinterpret_cast<const FloatRun<V>*>(a.bias + c);
+#pragma unroll
+    for (int i = 0; i < V; ++i) b[i] = r.v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) b[i] = 0.0f;
   }
 }
 // the input at place t of the sequence: a row, a row of the state, or zero
@@ -80,13 +95,16 @@ __device__ __forceinline__ int64_t state_of(const int32_t* idx, int n_states, in
   return i >= 0 && i < n_states ? i : -1;
 }
 
-template <class T, int V, int W>
+// WIDE: a wavefront's threads are all at one segment.
+template <class T, int V, int W, bool WIDE>
 __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
   const int per_y = 256 / a.per_x, col_tiles = (a.d + a.per_x * V - 1) / (a.per_x * V);
   const int c = ((int)(blockIdx.x % col_tiles) * a.per_x + (int)threadIdx.x % a.per_x) * V;
-  const int64_t item = (int64_t)(blockIdx.x / col_tiles) * per_y + threadIdx.x / a.per_x;
+  const int item0 = (int)(blockIdx.x / col_tiles) * per_y, item = item0 + (int)threadIdx.x / a.per_x;
+  const int s0 = seg_find(a.q, item0, a.bits);
   if (c >= a.d || item >= a.items) return;
-  const Piece p = piece_at(a.q, item, CONV_SEG);
+  const int at = WIDE ? __builtin_amdgcn_readfirstlane(item) : item;
+  const Piece p = piece_of(a.q, at, a.bits, seg_find_from(a.q, at, a.bits, s0));
   if (p.none) return;
   const int64_t state = state_of(a.state_idx, a.n_states, p.s);
   float w[W][V], b[V], win[W][V];
@@ -102,17 +120,39 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
       conv_input<T, V>(a, p.r, state, p.t0 - (a.width - 1) + j, c, v);
       shift_in<V, W>(win, v);
     }
-  for (int t = p.t0; t < p.t1; ++t) {
+  // rows are asked for AHEAD before their use
+  const int64_t step = a.q.newest_first ? -1 : 1;
+  const T* x = static_cast<const T*>(a.x) + seq_row(a.q, p.r, p.t0) * a.ld_x + c;
+  T* y = static_cast<T*>(a.y) + seq_row(a.q, p.r, p.t0) * a.ld_y + c;
+  Pack<T, V> next[AHEAD];
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u)
+    if (p.t0 + u < p.t1) next[u] = *reinterpret_cast<const Pack<T, V>*>(x + u * step * a.ld_x);
+  const bool silu = a.silu != 0;
+  auto row = [&](int u) {
     float v[V], pre[V];
-    const int64_t row = seq_row(a.q, p.r, t);
-    load_pack<T, V>(static_cast<const T*>(a.x) + row * a.ld_x + c, v);
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (float)next[u].v[i];
     shift_in<V, W>(win, v);
     conv_sum<V, W>(a, win, w, b, pre);
-    if (a.silu)
 #pragma unroll
-      for (int i = 0; i < V; ++i) pre[i] *= sigmoid(pre[i]);
-    store_pack<T, V>(static_cast<T*>(a.y) + row * a.ld_y + c, pre);
+    for (int i = 0; i < V; ++i) pre[i] *= silu ? sigmoid(pre[i]) : 1.0f;
+    store_pack<T, V>(y + u * step * a.ld_y, pre);
+  };
+  int t = p.t0;
+  for (; t + AHEAD <= p.t1; t += AHEAD) {   // whole groups
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      row(u);
+      const int ahead = min(u + AHEAD, p.t1 - 1 - t);   // (past the end: a row that is there)
+      next[u] = *reinterpret_cast<const Pack<T, V>*>(x + ahead * step * a.ld_x);
+    }
+    x += AHEAD * step * a.ld_x;
+    y += AHEAD * step * a.ld_y;
   }
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u)
+    if (t + u < p.t1) row(u);
   if (!p.last) return;
   float zero[V] = {};
   for (int t = p.r.len; t < p.r.slot; ++t) store_pack<T, V>(static_cast<T*>(a.y) + (p.r.begin + t) * a.ld_y + c, zero);
@@ -158,7 +198,7 @@ __global__ __launch_bounds__(256) void conv_step_kernel(ConvArgs a) {
     }
 }
 
-template <class T, int V, int W>
+template <class T, int V, int W, bool WIDE>
 __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
   __shared__ float acc[256 * V];
   const int per_y = 256 / a.per_x, col_tiles = (a.d + a.per_x * V - 1) / (a.per_x * V);
@@ -175,8 +215,11 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
   }
   if (on) conv_taps<V, W>(a, c, w, b);
   const int halo = a.width - 1;
-  for (int64_t item = (int64_t)worker * per_y + ty; on && item < a.items; item += (int64_t)workers * per_y) {
-    const Piece p = piece_at(a.q, item, CONV_SEG);
+  for (int64_t item0 = (int64_t)worker * per_y; item0 < a.items; item0 += (int64_t)workers * per_y) {
+    const int s0 = seg_find(a.q, (int)item0, a.bits), item = (int)item0 + ty;
+    if (!on || item >= a.items) continue;
+    const int at = WIDE ? __builtin_amdgcn_readfirstlane(item) : item;
+    const Piece p = piece_of(a.q, at, a.bits, seg_find_from(a.q, at, a.bits, s0));
     if (p.none) continue;
     const int64_t state = state_of(a.state_idx, a.n_states, p.s);
     float win[W][V], gw[W][V];
@@ -191,24 +234,36 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
         conv_input<T, V>(a, p.r, state, p.t0 - halo + j, c, v);
         shift_in<V, W>(win, v);
       }
-    // g[t] of the segment's events and of the `halo` behind them completes dx[t - halo]
-    for (int t = p.t0; t < p.t1 + halo; ++t) {
-      float g[V];
-      if (t < p.r.len) {
-        float v[V], pre[V];
-        const int64_t row = seq_row(a.q, p.r, t);
-        load_pack<T, V>(static_cast<const T*>(a.x) + row * a.ld_x + c, v);
-        load_pack<T, V>(static_cast<const T*>(a.dy) + row * a.ld_dy + c, g);
-        shift_in<V, W>(win, v);
-        if (a.silu) {
-          conv_sum<V, W>(a, win, w, b, pre);
+    // g[t] of the segment's events and of the `halo` behind them completes dx[t - halo].  Behind the sequence's end g is zero.
+    const bool silu = a.silu != 0;
+    const int t_end = min(p.t1 + halo, p.r.len);   // events that g is formed of
+    const int64_t step = a.q.newest_first ? -1 : 1;
+    const T* x = static_cast<const T*>(a.x) + seq_row(a.q, p.r, p.t0) * a.ld_x + c;
+    const T* dy = static_cast<const T*>(a.dy) + seq_row(a.q, p.r, p.t0) * a.ld_dy + c;
+    T* dx = static_cast<T*>(a.y) + seq_row(a.q, p.r, p.t0) * a.ld_y + c;
+    Pack<T, V> nx[AHEAD], ndy[AHEAD];
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
-            const float sg = sigmoid(pre[i]);
-            g[i] *= sg * (1.0f + pre[i] * (1.0f - sg));
-          }
+    for (int u = 0; u < AHEAD; ++u)
+      if (p.t0 + u < t_end) {
+        nx[u] = *reinterpret_cast<const Pack<T, V>*>(x + u * step * a.ld_x);
+        ndy[u] = *reinterpret_cast<const Pack<T, V>*>(dy + u * step * a.ld_dy);
+      }
+    // one event; INSIDE: it is the segment's own, and dx[t - halo] as well
+    auto event = [&](auto inside, int t, int u) {
+      constexpr bool INSIDE = decltype(inside)::value;
+      float g[V];
+      if (INSIDE || t < t_end) {
+        float v[V], pre[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) { v[i] = (float)nx[u].v[i]; g[i] = (float)ndy[u].v[i]; }
+        shift_in<V, W>(win, v);
+        conv_sum<V, W>(a, win, w, b, pre);
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const float sg = sigmoid(pre[i]);
+          g[i] *= silu ? sg * fmaf(pre[i], 1.0f - sg, 1.0f) : 1.0f;
         }
-        if (t < p.t1) {
+        if (INSIDE || t < p.t1) {
 #pragma unroll
           for (int j = 0; j < W; ++j)
             if (W != CONV_ANY || j >= W - a.width)
@@ -222,28 +277,49 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
         for (int i = 0; i < V; ++i) g[i] = 0.0f;
       }
       shift_in<V, W>(gw, g);
-      const int u = t - halo;
-      if (u >= p.t0 && u < p.t1) {
-        // dx[u] = sum over m of w[width - 1 - m] g[u + m]; g[u + m] is gw[W - width + m]
+      if (INSIDE || (t >= p.t0 + halo && t < p.t1 + halo)) {
+        // dx[t - halo] = sum over m of w[width - 1 - m] g[t - halo + m]: gw[j] is that with m = j - (W - width), its tap's place 2 W - 1 - width - j
         float o[V] = {};
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-          if (W == CONV_ANY && j < W - a.width) continue;
-          // gw[j] is g[u + m] with m = j - (W - width); its tap is w[W - 1 - m]
-          if constexpr (W != CONV_ANY) {
+        for (int j = 0; j < W; ++j)
 #pragma unroll
-            for (int i = 0; i < V; ++i) o[i] = fmaf(w[W - 1 - j][i], gw[j][i], o[i]);
-          } else {
+          for (int k = W != CONV_ANY ? W - 1 - j : 0; k < (W != CONV_ANY ? W - j : W); ++k)
+            if (W != CONV_ANY || (j >= W - a.width && k == 2 * W - 1 - a.width - j))
 #pragma unroll
-            for (int jj = 0; jj < W; ++jj)
-              if (jj == 2 * W - 1 - a.width - j)
-#pragma unroll
-                for (int i = 0; i < V; ++i) o[i] = fmaf(w[jj][i], gw[j][i], o[i]);
-          }
-        }
-        store_pack<T, V>(static_cast<T*>(a.y) + seq_row(a.q, p.r, u) * a.ld_y + c, o);
+              for (int i = 0; i < V; ++i) o[i] = fmaf(w[k][i], gw[j][i], o[i]);
+        store_pack<T, V>(dx + (u - halo) * step * a.ld_y, o);
       }
+    };
+    auto ask = [&](int t4, int u) {
+      const int ahead = min(u + AHEAD, t_end - 1 - t4);   // (past the end: a row that is there)
+      nx[u] = *reinterpret_cast<const Pack<T, V>*>(x + ahead * step * a.ld_x);
+      ndy[u] = *reinterpret_cast<const Pack<T, V>*>(dy + ahead * step * a.ld_dy);
+    };
+    auto on_to = [&]() {
+      x += AHEAD * step * a.ld_x;
+      dy += AHEAD * step * a.ld_dy;
+      dx += AHEAD * step * a.ld_y;
+    };
+    int t4 = p.t0;
+    auto border = [&]() {   // a group that is not all inside
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        if (t4 + u < p.t1 + halo) event(std::false_type(), t4 + u, u);
+        if (t4 + AHEAD < t_end) ask(t4, u);
+      }
+      on_to();
+      t4 += AHEAD;
+    };
+    while (t4 < p.t0 + halo && t4 < p.t1 + halo) border();
+    for (; t4 + AHEAD <= p.t1; t4 += AHEAD) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        event(std::true_type(), t4 + u, u);
+        ask(t4, u);
+      }
+      on_to();
     }
+    while (t4 < p.t1 + halo) border();
     if (p.last) {
       float zero[V] = {};
       for (int t = p.r.len; t < p.r.slot; ++t) store_pack<T, V>(static_cast<T*>(a.y) + (p.r.begin + t) * a.ld_y + c, zero);
@@ -281,7 +357,23 @@ static int conv_pack(int dtype, int d, int64_t rows, const void* const* p, const
   return 1;
 }
 
+// f(T(), V, W) for a pack of V values
 template <class F> static void conv_shape(int dtype, int pack, int width, F f) {
+  with_type(dtype, [&](auto t) {
+    auto by_width = [&](auto v) {
+      if (width == 2) f(t, v, std::integral_constant<int, 2>());
+      else if (width == 3) f(t, v, std::integral_constant<int, 3>());
+      else if (width == 4) f(t, v, std::integral_constant<int, 4>());
+      else f(t, v, std::integral_constant<int, CONV_ANY>());
+    };
+    if constexpr (sizeof(t) == 2)
+      if (pack == 8) return by_width(std::integral_constant<int, 8>());
+    if (pack >= 4) by_width(std::integral_constant<int, 4>());
+    else by_width(std::integral_constant<int, 1>());
+  });
+}
+// The same without packs of eight values, with which the backward pass has two wavefronts to a vector unit instead of three
+template <class F> static void conv_shape4(int dtype, int pack, int width, F f) {
   with_type(dtype, [&](auto t) {
     auto by_width = [&](auto v) {
       if (width == 2) f(t, v, std::integral_constant<int, 2>());
@@ -292,6 +384,15 @@ template <class F> static void conv_shape(int dtype, int pack, int width, F f) {
     if (pack >= 4) by_width(std::integral_constant<int, 4>());
     else by_width(std::integral_constant<int, 1>());
   });
+}
+
+// Rows of a segment, 2^4 to 2^6: as many as leave `waves` wavefronts with four rows each on their way.  What is read
+// twice is 5 per cent with 64 rows and four taps, 20 per cent (out of the L2) with 16.
+static int conv_bits(const tgnn_seqs& q, int d, int v, int waves) {
+  const int64_t rows = q.indptr == nullptr ? (int64_t)q.n_seqs * q.max_len : q.n_rows, packs = (d + v - 1) / v;
+  int bits = 6;
+  while (bits > 4 && (rows >> bits) * packs < (int64_t)waves * 64) --bits;
+  return bits;
 }
 
 static int conv_columns(int d, int v) {   // threads of a workgroup along the columns: a power of two, at most all
@@ -308,7 +409,8 @@ int check_seqs(const tgnn_seqs* q) {
   if (!aligned_to(q->indptr, 8) || !aligned_to(q->cnt, 4)) return set_error(TGNN_E_MISALIGNED, "indptr or cnt is not aligned to its type");
   if (q->indptr == nullptr && (int64_t)q->n_seqs * q->max_len > q->n_rows)
     return set_error(TGNN_E_OUT_OF_RANGE, "%d sequences of %d rows do not fit %lld rows", q->n_seqs, q->max_len, (long long)q->n_rows);
-  if (q->n_rows >= (int64_t(1) << 34)) return set_error(TGNN_E_OUT_OF_RANGE, "%lld rows", (long long)q->n_rows);
+  if (q->n_rows >= (int64_t(1) << 33) || seg_total(*q, MIN_SEG_BITS) > INT_MAX)   // (segments are numbered by 31 bits)
+    return set_error(TGNN_E_OUT_OF_RANGE, "%lld rows in %d sequences", (long long)q->n_rows, q->n_seqs);
   return TGNN_OK;
 }
 
@@ -360,8 +462,7 @@ extern "C" int32_t tgnn_causal_conv_fwd(const tgnn_seqs* seqs, int32_t dtype, in
   ConvArgs a = {};
   a.q = *seqs; a.x = x; a.w = weight; a.bias = bias; a.y = y;
   a.state_in = width > 1 ? state_in : nullptr; a.state_out = width > 1 ? state_out : nullptr; a.state_idx = state_idx;
-  a.ld_x = ld_x; a.ld_y = ld_y; a.items = seg_total(*seqs, CONV_SEG);
-  a.d = d; a.width = width; a.n_states = n_states; a.silu = silu != 0;
+  a.ld_x = ld_x; a.ld_y = ld_y; a.d = d; a.width = width; a.n_states = n_states; a.silu = silu != 0;
   const void* p[] = {x, y, a.state_in, a.state_out};
   const int64_t ld[] = {ld_x, ld_y, d, d};
   const int pack = conv_pack(dtype, d, seqs->n_rows, p, ld, 4);
@@ -369,11 +470,15 @@ extern "C" int32_t tgnn_causal_conv_fwd(const tgnn_seqs* seqs, int32_t dtype, in
   conv_shape(dtype, pack, width, [&](auto t, auto v, auto wd) {
     using T = decltype(t);
     constexpr int V = decltype(v)::value, W = decltype(wd)::value;
+    a.bits = conv_bits(*seqs, d, V, 4096);
+    a.items = seg_total(*seqs, a.bits);
     a.per_x = conv_columns(d, V);
     const int per_y = 256 / a.per_x, tiles = (d + a.per_x * V - 1) / (a.per_x * V);
     unsigned grid;
     rc = conv_grid((a.items + per_y - 1) / per_y, tiles, &grid);
-    if (rc == TGNN_OK) hipLaunchKernelGGL((conv_fwd_kernel<T, V, W>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    if (rc != TGNN_OK) return;
+    if (a.per_x >= 64) hipLaunchKernelGGL((conv_fwd_kernel<T, V, W, true>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    else hipLaunchKernelGGL((conv_fwd_kernel<T, V, W, false>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
   });
   if (rc != TGNN_OK) return rc;
   TGNN_LAUNCH_CHECK();
@@ -448,20 +553,23 @@ extern "C" int32_t tgnn_causal_conv_bwd(const tgnn_seqs* seqs, int32_t dtype, in
   ConvArgs a = {};
   a.q = *seqs; a.x = x; a.dy = dy; a.w = weight; a.bias = bias; a.y = dx; a.part = weights ? static_cast<float*>(workspace) : nullptr;
   a.state_in = width > 1 ? state_in : nullptr; a.state_idx = state_idx;
-  a.ld_x = ld_x; a.ld_dy = ld_dy; a.ld_y = ld_dx; a.items = seg_total(*seqs, CONV_SEG);
+  a.ld_x = ld_x; a.ld_dy = ld_dy; a.ld_y = ld_dx;
   a.d = d; a.width = width; a.n_states = n_states; a.silu = silu != 0;
   const void* p[] = {x, dy, dx, a.state_in};
   const int64_t ld[] = {ld_x, ld_dy, ld_dx, d};
   const int pack = conv_pack(dtype, d, seqs->n_rows, p, ld, 4);
   int64_t workers = 0;
   if (seqs->n_seqs > 0) {
-    conv_shape(dtype, pack, width, [&](auto t, auto v, auto wd) {
+    conv_shape4(dtype, pack, width, [&](auto t, auto v, auto wd) {
       using T = decltype(t);
       constexpr int V = decltype(v)::value, W = decltype(wd)::value;
+      a.bits = conv_bits(*seqs, d, V, 3072);
+      a.items = seg_total(*seqs, a.bits);
       a.per_x = conv_columns(d, V);
       const int per_y = 256 / a.per_x, tiles = (d + a.per_x * V - 1) / (a.per_x * V);
       workers = std::min<int64_t>((a.items + per_y - 1) / per_y, std::max(1, CONV_GRID / tiles));
-      hipLaunchKernelGGL((conv_bwd_kernel<T, V, W>), dim3((unsigned)(workers * tiles)), dim3(256), 0, s, a);
+      if (a.per_x >= 64) hipLaunchKernelGGL((conv_bwd_kernel<T, V, W, true>), dim3((unsigned)(workers * tiles)), dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((conv_bwd_kernel<T, V, W, false>), dim3((unsigned)(workers * tiles)), dim3(256), 0, s, a);
     });
     TGNN_LAUNCH_CHECK();
   }

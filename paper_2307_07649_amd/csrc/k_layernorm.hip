@@ -11,6 +11,8 @@
 // and leaves one partial row.
 #include <math.h>
 
+#include <algorithm>
+
 #include "ops_device.h"
 
 namespace tgnn {
@@ -41,50 +43,73 @@ struct NormArgs {
   float eps;
 };
 
+// V weights from column c on, or `other` ones
+template <int V> __device__ __forceinline__ void load_weights(const float* p, int c, float other, float (&w)[V]) {
+  if (p != nullptr) {
+    const FloatRun<V> r = *reinterpret_cast<const FloatRun<V>*>(p + c);
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = r.v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = other;
+  }
+}
+
+// A group of threads walks over rows with the weights of its columns in registers and the next row on its way.
 template <class T, int V, int G, int K>
 __global__ __launch_bounds__(256) void norm_fwd_kernel(NormArgs a) {
   __shared__ float parts[4];
+  constexpr int GROUPS = 256 / G;
   const int c0 = (threadIdx.x % G) * V;
-  const int64_t row = (int64_t)blockIdx.x * (256 / G) + threadIdx.x / G;
-  if (G <= 64 && row >= a.rows) return;   // (whole groups; with a workgroup per row there is none too many)
-  const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-  float v[K][V];
-#pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int c = c0 + k * G * V;
-    if (c < a.cols) load_pack<T, V>(x + c, v[k]);
-    else
-#pragma unroll
-      for (int i = 0; i < V; ++i) v[k][i] = 0.0f;
-  }
-  float sum = 0.0f;
+  const float inv = 1.0f / (float)a.cols;
+  float w[K][V], b[K][V];
 #pragma unroll
   for (int k = 0; k < K; ++k)
+    if (c0 + k * G * V < a.cols) {
+      load_weights<V>(a.weight, c0 + k * G * V, 1.0f, w[k]);
+      load_weights<V>(a.bias, c0 + k * G * V, 0.0f, b[k]);
+    }
+  const T* x = static_cast<const T*>(a.x) + c0;
+  T* y = static_cast<T*>(a.y) + c0;
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  int64_t row = (int64_t)blockIdx.x * GROUPS + threadIdx.x / G;
+  Pack<T, V> next[K];
+  auto ask = [&](int64_t r) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) sum += v[k][i];
-  const float mean = row_sum<G>(sum, parts) / (float)a.cols;
-  sum = 0.0f;
+    for (int k = 0; k < K; ++k)
+      if (c0 + k * G * V < a.cols) next[k] = *reinterpret_cast<const Pack<T, V>*>(x + r * a.ld_x + k * G * V);
+  };
+  if (row < a.rows) ask(row);
+  for (; row < a.rows; row += step) {
+    float v[K][V], sum = 0.0f;
 #pragma unroll
-  for (int k = 0; k < K; ++k)
-    if (c0 + k * G * V < a.cols)
+    for (int k = 0; k < K; ++k)
 #pragma unroll
-      for (int i = 0; i < V; ++i) sum += (v[k][i] - mean) * (v[k][i] - mean);
-  const float rstd = 1.0f / sqrtf(row_sum<G>(sum, parts) / (float)a.cols + a.eps);
-  if (threadIdx.x % G == 0) {
-    if (a.out_mean) a.out_mean[row] = mean;
-    if (a.out_rstd) a.out_rstd[row] = rstd;
-  }
-  T* y = static_cast<T*>(a.y) + row * a.ld_y;
+      for (int i = 0; i < V; ++i) {
+        v[k][i] = c0 + k * G * V < a.cols ? (float)next[k].v[i] : 0.0f;
+        sum += v[k][i];
+      }
+    if (row + step < a.rows) ask(row + step);
+    const float mean = row_sum<G>(sum, parts) * inv;
+    sum = 0.0f;
 #pragma unroll
-  for (int k = 0; k < K; ++k) {
-    const int c = c0 + k * G * V;
-    if (c >= a.cols) continue;
-    float w[V], b[V];
+    for (int k = 0; k < K; ++k)
+      if (c0 + k * G * V < a.cols)
 #pragma unroll
-    for (int i = 0; i < V; ++i) { w[i] = a.weight ? a.weight[c + i] : 1.0f; b[i] = a.bias ? a.bias[c + i] : 0.0f; }
+        for (int i = 0; i < V; ++i) sum += (v[k][i] - mean) * (v[k][i] - mean);
+    const float rstd = 1.0f / sqrtf(row_sum<G>(sum, parts) * inv + a.eps);
+    if (threadIdx.x % G == 0) {
+      if (a.out_mean) a.out_mean[row] = mean;
+      if (a.out_rstd) a.out_rstd[row] = rstd;
+    }
 #pragma unroll
-    for (int i = 0; i < V; ++i) w[i] = (v[k][i] - mean) * rstd * w[i] + b[i];
-    store_pack<T, V>(y + c, w);
+    for (int k = 0; k < K; ++k) {
+      if (c0 + k * G * V >= a.cols) continue;
+      float o[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) o[i] = (v[k][i] - mean) * rstd * w[k][i] + b[k][i];
+      store_pack<T, V>(y + row * a.ld_y + k * G * V, o);
+    }
   }
 }
 
@@ -117,27 +142,38 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormArgs a) {
   const int c0 = (threadIdx.x % G) * V, group = threadIdx.x / G;
   float w[K][V], dw[K][V], db[K][V];
 #pragma unroll
-  for (int k = 0; k < K; ++k)
+  for (int k = 0; k < K; ++k) {
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const int c = c0 + k * G * V + i;
-      w[k][i] = c < a.cols ? (a.weight ? a.weight[c] : 1.0f) : 0.0f;
-      dw[k][i] = db[k][i] = 0.0f;
-    }
+    for (int i = 0; i < V; ++i) w[k][i] = dw[k][i] = db[k][i] = 0.0f;   // (columns beyond the row weigh nothing)
+    if (c0 + k * G * V < a.cols) load_weights<V>(a.weight, c0 + k * G * V, 1.0f, w[k]);
+  }
   const float inv = 1.0f / (float)a.cols;
-  for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < a.rows; row += (int64_t)gridDim.x * GROUPS) {
-    const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-    const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
-    const float mean = a.mean[row], rstd = a.rstd[row];
+  const T* x = static_cast<const T*>(a.x) + c0;
+  const T* dy = static_cast<const T*>(a.dy) + c0;
+  T* dx = static_cast<T*>(a.y) + c0;
+  const int64_t step = (int64_t)gridDim.x * GROUPS;
+  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+  Pack<T, V> nx[K], ndy[K];
+  float next_mean = 0.0f, next_rstd = 0.0f;
+  auto ask = [&](int64_t r) {
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (c0 + k * G * V < a.cols) {
+        nx[k] = *reinterpret_cast<const Pack<T, V>*>(x + r * a.ld_x + k * G * V);
+        ndy[k] = *reinterpret_cast<const Pack<T, V>*>(dy + r * a.ld_dy + k * G * V);
+      }
+    next_mean = a.mean[r];
+    next_rstd = a.rstd[r];
+  };
+  if (row < a.rows) ask(row);
+  for (; row < a.rows; row += step) {
+    const float mean = next_mean, rstd = next_rstd;
     float xh[K][V], g[K][V];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      const int c = c0 + k * G * V;
-      if (c < a.cols) {
-        load_pack<T, V>(x + c, xh[k]);
-        load_pack<T, V>(dy + c, g[k]);
-      }
-    }
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) { xh[k][i] = (float)nx[k].v[i]; g[k][i] = (float)ndy[k].v[i]; }
+    if (row + step < a.rows) ask(row + step);
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -155,15 +191,13 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormArgs a) {
     }
     s1 = row_sum<G>(s1, parts) * inv;
     s2 = row_sum<G>(s2, parts) * inv;
-    T* dx = static_cast<T*>(a.y) + row * a.ld_y;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int c = c0 + k * G * V;
-      if (c >= a.cols) continue;
+      if (c0 + k * G * V >= a.cols) continue;
       float o[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) o[i] = rstd * (g[k][i] - s1 - xh[k][i] * s2);
-      store_pack<T, V>(dx + c, o);
+      store_pack<T, V>(dx + row * a.ld_y + k * G * V, o);
     }
   }
   if (a.part == nullptr) return;
@@ -242,7 +276,9 @@ static int norm_pack(int dtype, int cols, int64_t rows, const void* const* p, co
   return 1;
 }
 
-constexpr int NORM_GRID = 1024;       // workgroups of the backward pass (partial rows of dw and db)
+constexpr int NORM_FWD_GRID = 2048;   // workgroups of the forward pass: eight to a compute unit
+constexpr int NORM_GRID = 1024;       // workgroups of the backward pass (partial rows of dw and db), 768 where rows are
+                                      // so wide that the partial rows' way counts and registers allow three to a compute unit
 constexpr int NORM_WIDE_PARTS = 64;   // the same where rows are wider than the registers
 
 // f(G, K) for the smallest group of threads that covers `packs` packs of a row; false: none does
@@ -268,7 +304,8 @@ template <class T, class F> static void norm_width(int pack, F f) {   // f(V)
 }
 
 static int64_t norm_grid(int64_t rows, int cols) {
-  return rows < NORM_GRID ? (rows > 0 ? rows : 1) : NORM_GRID;
+  const int64_t most = cols > 1024 ? 768 : NORM_GRID;
+  return rows < most ? (rows > 0 ? rows : 1) : most;
 }
 
 static int check_rows(const char* name, const void* p, int64_t ld, int64_t rows, int cols, int dtype) {
@@ -321,7 +358,8 @@ extern "C" int32_t tgnn_layer_norm_fwd(int32_t dtype, int64_t n_rows, int32_t n_
       constexpr int V = decltype(v)::value;
       const bool fits = norm_shape((n_cols + V - 1) / V, [&](auto g, auto k) {
         constexpr int G = decltype(g)::value, K = decltype(k)::value, PER = 256 / G;
-        hipLaunchKernelGGL((norm_fwd_kernel<T, V, G, K>), dim3((unsigned)((n_rows + PER - 1) / PER)), dim3(256), 0, s, a);
+        const int64_t blocks = std::min<int64_t>((n_rows + PER - 1) / PER, NORM_FWD_GRID);
+        hipLaunchKernelGGL((norm_fwd_kernel<T, V, G, K>), dim3((unsigned)blocks), dim3(256), 0, s, a);
       });
       if (!fits) hipLaunchKernelGGL((norm_fwd_wide_kernel<T>), dim3((unsigned)n_rows), dim3(256), 0, s, a);
     });

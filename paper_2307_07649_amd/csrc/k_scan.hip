@@ -34,7 +34,8 @@
 
 namespace tgnn {
 
-constexpr int CHUNK = 32;               // events between two saved states
+constexpr int CHUNK_BITS = 5, CHUNK = 32;   // events between two saved states
+constexpr int SUM_BITS = 3;                 // rows that a workgroup adds up the column tiles' parts of dB and dC of
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct ScanArgs {
@@ -51,7 +52,7 @@ struct ScanArgs {
   float* part_bc;                       // [column tiles of a group, rows, 2, groups n]; NULL: dB and dC are written directly
   int64_t ld_x, ld_dt, ld_b, ld_c, ld_z, ld_dy, ld_y, ld_dx, ld_ddt, ld_dz, ld_db, ld_dc, items;
   int d, n, groups, dg, n_states, softplus;
-  int seg;                              // events of a segment, 0: sequences are not cut
+  int bits;                             // a segment has 2^bits events; WHOLE: sequences are not cut
   int tiles;                            // column tiles of a group
 };
 
@@ -124,14 +125,14 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a) {
   const unsigned w4 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wave = blockIdx.x * 4 + w4;
   const unsigned all = (unsigned)(a.groups * a.tiles), item = wave / all, tile = wave - item * all;
   if (item >= a.items) return;
-  const Piece p = piece_at(a.q, item, a.seg);
+  const Piece p = piece_at(a.q, (int)item, a.bits);
   if (p.none || (MODE == SCAN_PART && p.last) || (BACK && p.t0 == 0)) return;
   const int g = tile / a.tiles, col = (tile - g * a.tiles) * 64 + lane;
   const unsigned c = g * a.dg + min(col, a.dg - 1);
   const int64_t state = state_of(a, p.s);
   float A[NP], h[NP];
   load_states<NP>(a.A + (int64_t)c * a.n, a.n, A);
-  if (!PART && a.seg != 0) load_states<NP>(a.seg_state + (p.slot * a.d + c) * a.n, a.n, h);
+  if (!PART && a.bits != WHOLE) load_states<NP>(a.seg_state + ((int64_t)p.slot * a.d + c) * a.n, a.n, h);
   else if (!PART && state >= 0 && a.state_in != nullptr) load_states<NP>(a.state_in + (state * a.d + c) * a.n, a.n, h);
   else
 #pragma unroll
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a) {
   };
   // whole groups, and what is left of them at the end (of the segment: the first thing on the way back)
   const int n_ev = p.t1 - p.t0, whole = n_ev / 4, left = n_ev & 3;
-  float* saved = !PART && a.saved != nullptr ? a.saved + ((seg_base(a.q, p.s, CHUNK) + p.t0 / CHUNK) * a.d + c) * a.n : nullptr;
+  float* saved = !PART && a.saved != nullptr ? a.saved + ((int64_t)(seg_base(a.q, p.s, CHUNK_BITS) + p.t0 / CHUNK) * a.d + c) * a.n : nullptr;
   const int64_t saved_step = (int64_t)a.d * a.n;
   E next;
   if (left != 0 && (BACK || whole == 0)) ask(p.t0 + 4 * whole, left, next);
@@ -234,8 +235,8 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a) {
     work(p.t0 + 4 * whole, left, next);
   }
   if (PART) {
-    store_states<NP>(a.seg_state + (p.slot * a.d + c) * a.n, a.n, h);
-    a.seg_delta[p.slot * a.d + c] = total;
+    store_states<NP>(a.seg_state + ((int64_t)p.slot * a.d + c) * a.n, a.n, h);
+    a.seg_delta[(int64_t)p.slot * a.d + c] = total;
   }
   if (OUT && p.last) {
     for (int t = p.r.len; t < p.r.slot; ++t) (static_cast<T*>(a.y) + (p.r.begin + t) * a.ld_y)[c] = (T)0.0f;
@@ -258,8 +259,8 @@ __global__ __launch_bounds__(256) void scan_chain_kernel(ScanArgs a) {
   const bool on = e < dn;
   const int c = on ? (int)(e / a.n) : 0;
   const Seq r = seq_at(a.q, s);
-  const int64_t base = seg_base(a.q, s, a.seg);
-  const int count = r.len > 0 ? (int)(((int64_t)r.len + a.seg - 1) / a.seg) : 1;
+  const int64_t base = seg_base(a.q, s, a.bits);
+  const int count = seg_count(r.len, a.bits);
   const int64_t state = state_of(a, s);
   const float A = on ? a.A[e] * LOG2E : 0.0f;
   // segment k in the order of the recurrence; the last one's part was not formed (and is not needed)
@@ -347,11 +348,8 @@ template <int NP> __device__ __forceinline__ void column_sums(const float (&v)[4
 __device__ __forceinline__ int event_of_sum(int lane) { return 2 * (lane >> 5) + (lane >> 4 & 1); }
 
 // A workgroup: 16 columns per wavefront of one group, over the pieces worker, worker + workers, ...
-#ifndef OCC
-#define OCC 3
-#endif
 template <class T, int NP, bool USUAL>
-__global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bwd_kernel(ScanArgs a) {
+__global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_kernel(ScanArgs a) {
   constexpr int WAVES = bwd_waves(NP), THREADS = 64 * WAVES, N4 = 4 * NP, STAGE = CHUNK * N4 / THREADS > 0 ? CHUNK * N4 / THREADS : 1;
   constexpr bool AHEAD = STAGE <= 2;                 // the next chunk's B, C and states are asked for a chunk ahead
   __shared__ float bound[CHUNK / 4][THREADS * NP];   // a lane's states before every fourth event
@@ -376,20 +374,44 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bw
   const unsigned up = newest ? 3 - q : q;
   const unsigned ox = up * (unsigned)a.ld_x + c, odt = up * (unsigned)a.ld_dt + c, oz = up * (unsigned)a.ld_z + c, ody = up * (unsigned)a.ld_dy + c;
 
-  for (int64_t item = worker; item < a.items; item += workers) {
-    const Piece p = piece_at(a.q, item, a.seg);
-    if (p.none) continue;
+  // The next piece that has events; padding rows are cleared on the way.
+  int64_t item = worker;
+  auto advance = [&](Piece& p) -> bool {
+    for (; item < a.items; item += workers) {
+      p = piece_at(a.q, (int)item, a.bits);
+      if (p.none) continue;
+      if (p.last && p.r.slot > p.r.len) {
+        for (int t = p.r.len + q; on && t < p.r.slot; t += 4) {
+          const int64_t row = p.r.begin + t;
+          (static_cast<T*>(a.dx) + row * a.ld_dx)[c] = (T)0.0f;
+          (static_cast<T*>(a.ddt) + row * a.ld_ddt)[c] = (T)0.0f;
+          if (gated) (static_cast<T*>(a.dz) + row * a.ld_dz)[c] = (T)0.0f;
+        }
+        if (sub == 0)
+          for (int t = p.r.len + wave; t < p.r.slot; t += WAVES)
+            for (int n = lane; n < a.n; n += 64) {
+              const int64_t row = p.r.begin + t;
+              (static_cast<T*>(a.dB) + row * a.ld_db)[grp * a.n + n] = (T)0.0f;
+              (static_cast<T*>(a.dC) + row * a.ld_dc)[grp * a.n + n] = (T)0.0f;
+            }
+      }
+      if (p.t0 < p.t1) {
+        item += workers;
+        return true;
+      }
+    }
+    return false;
+  };
+  // The chunk in hand and the next one (of the same piece, or the last chunk of the next piece): its B, C and first states, and its
+  // first four events, are asked for while the one in hand is worked on.
+  {
+    Piece p, np;
+    bool more = advance(p);
+    int tb = more ? p.t0 + (p.t1 - 1 - p.t0) / CHUNK * CHUNK : 0;
     float g[NP];   // what reaches the state behind the event in hand from the events after it
-#pragma unroll
-    for (int i = 0; i < NP; ++i)
-      g[i] = a.seg != 0 && on && q * NP + i < a.n ? a.seg_state[(p.slot * a.d + c) * a.n + q * NP + i] : 0.0f;
-    const float* saved = a.saved + (seg_base(a.q, p.s, CHUNK) * a.d + c) * a.n + q * NP;
-    const int64_t saved_step = (int64_t)a.d * a.n;
-
-    // B, C and the first states of the chunk that begins at tb
     T rb[STAGE], rc[STAGE];
     float hn[NP];
-    auto ask_chunk = [&](int tb) {
+    auto ask_chunk = [&](const Piece& p, int tb) {
       const int n_ev = min(CHUNK, p.t1 - tb);
 #pragma unroll
       for (int r = 0; r < STAGE; ++r) {
@@ -401,14 +423,19 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bw
           rc[r] = (static_cast<const T*>(a.C) + row * a.ld_c)[grp * a.n + n];
         }
       }
-      const float* sv = saved + (tb / CHUNK) * saved_step;
+      const float* sv = a.saved + ((int64_t)(seg_base(a.q, p.s, CHUNK_BITS) + tb / CHUNK) * a.d + c) * a.n + q * NP;
 #pragma unroll
       for (int i = 0; i < NP; ++i) hn[i] = on && q * NP + i < a.n ? sv[i] : 0.0f;
     };
+    auto ask_back = [&](const Piece& p) {   // what reaches a piece from behind
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+        g[i] = a.bits != WHOLE && on && q * NP + i < a.n ? a.seg_state[((int64_t)p.slot * a.d + c) * a.n + q * NP + i] : 0.0f;
+    };
     struct Own { T x, dt, z, dy; };
-    auto low_row = [&](int t) { return p.r.begin + (newest ? p.r.len - 4 - t : t); };   // of the events t .. t + 3
-    auto ask = [&](int t, bool back, Own& v) {
-      const int64_t row = low_row(t);
+    auto low_row = [&](const Piece& p, int t) { return p.r.begin + (newest ? p.r.len - 4 - t : t); };   // of the events t .. t + 3
+    auto ask = [&](const Piece& p, int t, bool back, Own& v) {
+      const int64_t row = low_row(p, t);
       v.x = v.dt = v.z = v.dy = (T)0.0f;
       if (on && t + q < p.t1) {
         v.x = (static_cast<const T*>(a.x) + row * a.ld_x)[ox];
@@ -420,11 +447,15 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bw
       }
     };
 
-    const int tb0 = p.t1 > p.t0 ? p.t0 + (p.t1 - 1 - p.t0) / CHUNK * CHUNK : p.t0 - CHUNK;
-    if (AHEAD && tb0 >= p.t0) ask_chunk(tb0);
-    for (int tb = tb0; tb >= p.t0; tb -= CHUNK) {
+    Own nx;
+    if (more) {
+      if (AHEAD) ask_chunk(p, tb);
+      ask_back(p);
+      ask(p, tb, p.t1 - tb <= 4, nx);
+    }
+    while (more) {
       const int n_ev = min(CHUNK, p.t1 - tb), n_sub = (n_ev + 3) / 4;
-      if (!AHEAD) ask_chunk(tb);
+      if (!AHEAD) ask_chunk(p, tb);
 #pragma unroll
       for (int r = 0; r < STAGE; ++r)
         if (CHUNK * N4 >= THREADS || tid < CHUNK * N4) {
@@ -435,14 +466,12 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bw
 #pragma unroll
       for (int i = 0; i < NP; ++i) h[i] = hn[i];
       __syncthreads();
-      Own nx;
-      ask(tb, n_sub == 1, nx);
       // forward over the chunk: the state before every fourth event
 #pragma unroll
       for (int i = 0; i < NP; ++i) bound[0][tid * NP + i] = h[i];
       for (int j = 0; j + 1 < n_sub; ++j) {
         const Own v = nx;
-        ask(tb + 4 * j + 4, j + 2 == n_sub, nx);
+        ask(p, tb + 4 * j + 4, j + 2 == n_sub, nx);
         const float raw = (float)v.dt + bias, delta = soft ? softplus(raw) : raw, d2 = delta * LOG2E, in = delta * (float)v.x;
         const float d2s[4] = {quad_get<0>(d2), quad_get<1>(d2), quad_get<2>(d2), quad_get<3>(d2)};
         const float ins[4] = {quad_get<0>(in), quad_get<1>(in), quad_get<2>(in), quad_get<3>(in)};
@@ -454,11 +483,19 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bw
 #pragma unroll
         for (int i = 0; i < NP; ++i) bound[j + 1][tid * NP + i] = h[i];
       }
-      if (AHEAD && tb > p.t0) ask_chunk(tb - CHUNK);
+      const bool next_piece = tb == p.t0;
+      int next_tb = tb - CHUNK;
+      np = p;
+      if (next_piece) {
+        more = advance(np);
+        next_tb = more ? np.t0 + (np.t1 - 1 - np.t0) / CHUNK * CHUNK : 0;
+      }
+      if (AHEAD && more) ask_chunk(np, next_tb);
       // and back, four events at a time
       for (int j = n_sub - 1; j >= 0; --j) {
         const Own v = nx;
-        if (j > 0) ask(tb + 4 * j - 4, true, nx);
+        if (j > 0) ask(p, tb + 4 * j - 4, true, nx);
+        else if (more) ask(np, next_tb, np.t1 - next_tb <= 4, nx);
         const bool there = on && 4 * j + q < n_ev;
         const float x = (float)v.x, raw = (float)v.dt + bias, z = (float)v.z, dy = (float)v.dy;
         const float delta = there ? (soft ? softplus(raw) : raw) : 0.0f, sg = gated ? sigmoid(z) : 1.0f, gy = gated ? dy * z * sg : dy;
@@ -515,7 +552,7 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bw
         float dz = 0.0f;
         if (gated) dz = dy * fmaf(D, x, quad_scatter_sum(y, odd, high)) * (sg * fmaf(z, 1.0f - sg, 1.0f));
         if (there) {
-          const int64_t row = low_row(tb + 4 * j);
+          const int64_t row = low_row(p, tb + 4 * j);
           (static_cast<T*>(a.dx) + row * a.ld_dx)[up * (unsigned)a.ld_dx + c] = (T)fmaf(D, gy, delta * t1);
           (static_cast<T*>(a.ddt) + row * a.ld_ddt)[up * (unsigned)a.ld_ddt + c] = (T)draw;
           if (gated) (static_cast<T*>(a.dz) + row * a.ld_dz)[up * (unsigned)a.ld_dz + c] = (T)dz;
@@ -523,6 +560,7 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bw
           dbias += draw;
         }
       }
+      if (next_piece && more) ask_back(np);
       __syncthreads();
       for (int i = tid; i < n_ev * 2 * N4; i += THREADS) {
         const int kind = i >= n_ev * N4, at = kind ? i - n_ev * N4 : i, e = at / N4, n = at % N4;
@@ -536,21 +574,8 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bw
         else if (kind == 0) (static_cast<T*>(a.dB) + row * a.ld_db)[k] = (T)sum;
         else (static_cast<T*>(a.dC) + row * a.ld_dc)[k] = (T)sum;
       }
-    }
-    if (p.last) {   // padding rows
-      for (int t = p.r.len + q; on && t < p.r.slot; t += 4) {
-        const int64_t row = p.r.begin + t;
-        (static_cast<T*>(a.dx) + row * a.ld_dx)[c] = (T)0.0f;
-        (static_cast<T*>(a.ddt) + row * a.ld_ddt)[c] = (T)0.0f;
-        if (gated) (static_cast<T*>(a.dz) + row * a.ld_dz)[c] = (T)0.0f;
-      }
-      if (sub == 0)
-        for (int64_t i = tid; i < (int64_t)(p.r.slot - p.r.len) * a.n; i += THREADS) {
-          const int64_t row = p.r.begin + p.r.len + i / a.n;
-          const int k = grp * a.n + (int)(i % a.n);
-          (static_cast<T*>(a.dB) + row * a.ld_db)[k] = (T)0.0f;
-          (static_cast<T*>(a.dC) + row * a.ld_dc)[k] = (T)0.0f;
-        }
+      p = np;
+      tb = next_tb;
     }
   }
   if (a.part == nullptr) return;
@@ -572,7 +597,7 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? OCC : 1) void scan_bw
 // dB and dC of the rows of sequences: the column tiles' parts in order
 template <class T>
 __global__ __launch_bounds__(256) void scan_bc_sum_kernel(ScanArgs a) {
-  const Piece p = piece_at(a.q, blockIdx.x, CHUNK);
+  const Piece p = piece_at(a.q, (int)blockIdx.x, SUM_BITS);
   if (p.none) return;
   const int per = a.groups * a.n;
   for (int i = threadIdx.x; i < (p.t1 - p.t0) * 2 * per; i += 256) {
@@ -585,46 +610,119 @@ __global__ __launch_bounds__(256) void scan_bc_sum_kernel(ScanArgs a) {
   }
 }
 
-// One event of each of `items` nodes: LC neighbouring lanes have a column, NP states each, next to each other in memory.
-template <class T, int NP>
-__global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int lc_bits) {
-  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> lc_bits;
-  const int part = threadIdx.x & ((1 << lc_bits) - 1);
-  const bool on = i < a.items * a.d;
-  const int64_t row = on ? i / a.d : 0;
-  const int c = on ? (int)(i - row * a.d) : 0;
-  const int g = c / a.dg;
-  const int64_t state = state_of(a, (int)row);
-  const float x = (float)(static_cast<const T*>(a.x) + row * a.ld_x)[c];
-  const float raw = (float)(static_cast<const T*>(a.dt) + row * a.ld_dt)[c] + (a.bias ? a.bias[c] : 0.0f);
-  const float delta = a.softplus ? softplus(raw) : raw, in = delta * x, d2 = delta * LOG2E;
-  float y = 0.0f;
-  float h[NP];
-  const bool stored = state >= 0 && a.state_in != nullptr;
-  const int64_t s0 = (state * a.d + c) * a.n + part * NP;
+// One event of each of `items` rows, on the rows' states.  LC = 2^bits neighbouring lanes have a column, four states each, next to each
+// other in memory; a workgroup has 256 / LC columns of four rows, whose states are asked for together.  With four lanes and
+// more to a column (QUAD) every one of four neighbouring lanes forms the step size and the gate of one of the rows.  4,000
+// rows of 256 columns and 16 states, 131 MB of states in and out: 47 us; walking over the rows with the next four's states
+// on their way, 65 (138 registers, half the wavefronts).
+template <class T, bool QUAD>
+__global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int bits, int tiles) {
+  const int tile = blockIdx.x % tiles, part = threadIdx.x & ((1 << bits) - 1), q = threadIdx.x & 3;
+  const int64_t row0 = (int64_t)(blockIdx.x / tiles) * 4, last = a.items - 1;
+  const int col = tile * (256 >> bits) + (int)(threadIdx.x >> bits), c = min(col, a.d - 1), n0 = part * 4;
+  const bool on = col < a.d, whole = n0 + 4 <= a.n;
+  const int s0 = min(n0, a.n - 1), bc = c / a.dg * a.n + s0;   // (lanes without a state read another's)
+  auto floats = [&](const float* p, float (&v)[4]) {
+    if (whole) {
+      const FloatRun<4> r = *reinterpret_cast<const FloatRun<4>*>(p);
 #pragma unroll
-  for (int k = 0; k < NP; ++k) {
-    const int n = part * NP + k;
-    h[k] = 0.0f;
-    if (n >= a.n) continue;
-    const float h0 = stored ? a.state_in[s0 + k] : 0.0f;
-    const float B = (float)(static_cast<const T*>(a.B) + row * a.ld_b)[g * a.n + n], C = (float)(static_cast<const T*>(a.C) + row * a.ld_c)[g * a.n + n];
-    h[k] = fmaf(__builtin_amdgcn_exp2f(d2 * a.A[(int64_t)c * a.n + n]), h0, in * B);
-    y = fmaf(h[k], C, y);
-  }
-  for (int o = 1; o < 1 << lc_bits; o <<= 1) y += __shfl_xor(y, o);
-  if (!on) return;
-  if (state >= 0 && a.state_out != nullptr)
+      for (int i = 0; i < 4; ++i) v[i] = r.v[i];
+    } else {
 #pragma unroll
-    for (int k = 0; k < NP; ++k)
-      if (part * NP + k < a.n) a.state_out[s0 + k] = h[k];
-  if (part != 0) return;
-  y = fmaf(a.D ? a.D[c] : 0.0f, x, y);
-  if (a.z) {
-    const float z = (float)(static_cast<const T*>(a.z) + row * a.ld_z)[c];
-    y *= z * sigmoid(z);
+      for (int i = 0; i < 4; ++i) v[i] = n0 + i < a.n ? p[i] : 0.0f;
+    }
+  };
+  auto values = [&](const void* base, int64_t at, float (&v)[4]) {
+    const T* p = static_cast<const T*>(base) + at;
+    if (whole) {
+      const Run<T, 4> r = *reinterpret_cast<const Run<T, 4>*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = (float)r.v[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = n0 + i < a.n ? (float)p[i] : 0.0f;
+    }
+  };
+  float A[4], h[4][4], B[4][4], C[4][4], y[4];
+  int64_t state[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const int64_t row = min(row0 + e, last);
+    state[e] = state_of(a, (int)row);
+    if (state[e] >= 0 && a.state_in != nullptr) floats(a.state_in + (state[e] * a.d + c) * a.n + s0, h[e]);
+    else
+#pragma unroll
+      for (int i = 0; i < 4; ++i) h[e][i] = 0.0f;
+    values(a.B, row * a.ld_b + bc, B[e]);
+    values(a.C, row * a.ld_c + bc, C[e]);
   }
-  (static_cast<T*>(a.y) + row * a.ld_y)[c] = (T)y;
+  floats(a.A + (int64_t)c * a.n + s0, A);
+  const float bias = a.bias ? a.bias[c] : 0.0f, D = a.D ? a.D[c] : 0.0f;
+  struct Own { float x, d2, in, gate; };   // of one row
+  auto own = [&](int64_t r) {
+    const int64_t row = min(r, last);
+    Own o;
+    o.x = (float)(static_cast<const T*>(a.x) + row * a.ld_x)[c];
+    const float raw = (float)(static_cast<const T*>(a.dt) + row * a.ld_dt)[c] + bias, delta = a.softplus ? softplus(raw) : raw;
+    o.d2 = delta * LOG2E;
+    o.in = delta * o.x;
+    o.gate = 1.0f;
+    if (a.z) {
+      const float z = (float)(static_cast<const T*>(a.z) + row * a.ld_z)[c];
+      o.gate = z * sigmoid(z);
+    }
+    return o;
+  };
+  auto event = [&](int e, float d2, float in) {
+    y[e] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      h[e][i] = fmaf(__builtin_amdgcn_exp2f(d2 * A[i]), h[e][i], in * B[e][i]);
+      y[e] = fmaf(h[e][i], C[e][i], y[e]);
+    }
+  };
+  Own o[QUAD ? 1 : 4];
+  if constexpr (QUAD) {
+    o[0] = own(row0 + q);
+    event(0, quad_get<0>(o[0].d2), quad_get<0>(o[0].in));
+    event(1, quad_get<1>(o[0].d2), quad_get<1>(o[0].in));
+    event(2, quad_get<2>(o[0].d2), quad_get<2>(o[0].in));
+    event(3, quad_get<3>(o[0].d2), quad_get<3>(o[0].in));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      o[e] = own(row0 + e);
+      event(e, o[e].d2, o[e].in);
+    }
+  }
+  if (on && n0 < a.n && a.state_out != nullptr)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (row0 + e > last || state[e] < 0) continue;
+      float* p = a.state_out + (state[e] * a.d + c) * a.n + n0;
+      if (whole) {
+        FloatRun<4> r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.v[i] = h[e][i];
+        *reinterpret_cast<FloatRun<4>*>(p) = r;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n0 + i < a.n) p[i] = h[e][i];
+      }
+    }
+  if constexpr (QUAD) {
+    float sum = quad_scatter_sum(y, (q & 1) != 0, (q & 2) != 0);   // lane q: of row q
+    for (int s = 4; s < 1 << bits; s <<= 1) sum += __shfl_xor(sum, s);
+    if (on && part < 4 && row0 + q <= last) (static_cast<T*>(a.y) + (row0 + q) * a.ld_y)[c] = (T)(fmaf(D, o[0].x, sum) * o[0].gate);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float sum = y[e];
+      for (int s = 1; s < 1 << bits; s <<= 1) sum += __shfl_xor(sum, s);
+      if (on && part == 0 && row0 + e <= last) (static_cast<T*>(a.y) + (row0 + e) * a.ld_y)[c] = (T)(fmaf(D, o[e].x, sum) * o[e].gate);
+    }
+  }
 }
 
 // ---- host side ----
@@ -663,15 +761,16 @@ static ScanArgs scan_args(const tgnn_seqs* q, const tgnn_scan* p) {
 // Rows that a call's sequences hold at most, and the longest of them as far as the caller says
 static int64_t scan_rows(const tgnn_seqs& q) { return q.indptr == nullptr ? (int64_t)q.n_seqs * q.max_len : q.n_rows; }
 
-// Events of a segment (a multiple of CHUNK), 0: sequences are walked whole.  `units` wavefronts (forward) or workgroups
-// (backward) have a sequence between them, `spread` of them run side by side at full speed, `fill` times as many hide each other's
-// latencies.  Whole, a call takes as many steps as the longest sequence has events, or as all of them share out; in segments it
-// takes 1.8 times the shared work (every event once more for the segments' parts), some 40 steps' time for two more launches,
-// and the walk over one segment.
+// Bits of a segment's length, or WHOLE.  `units` wavefronts (forward) or workgroups (backward) have a sequence between them, `spread`
+// of them run side by side at full speed, `fill` times as many hide each other's latencies and even out the segments' lengths.  Whole, a call
+// takes as many steps as the longest sequence has events, or as all of them share out; in segments it takes 1.8 times the
+// shared work (every event once more for the segments' parts), some 40 steps' time for two more launches, and the walk over
+// one segment.
 static int scan_segment(const tgnn_seqs& q, int64_t units, int64_t spread, int64_t fill) {
   const int64_t rows = scan_rows(q), longest = std::min<int64_t>(q.max_len, rows), work = rows * units / spread;
-  const int64_t seg = std::min<int64_t>(std::max<int64_t>((work / fill + CHUNK - 1) / CHUNK * CHUNK, CHUNK), 4096);
-  return std::max(longest, work) > work + work * 4 / 5 + 40 + seg ? (int)seg : 0;
+  int bits = CHUNK_BITS;
+  while (bits < 12 && (int64_t(3) << bits) / 2 <= work / fill) ++bits;   // (the nearest power of two)
+  return std::max(longest, work) > work + work * 4 / 5 + 40 + (1 << bits) ? bits : WHOLE;
 }
 
 template <class F> static void scan_shape(int dtype, int n, F f) {   // f(T(), states of a lane that has them all)
@@ -694,21 +793,15 @@ struct Take {   // pieces of a workspace
   }
 };
 
-#ifndef FFILL
-#define FFILL 4
-#endif
-#ifndef BFILL
-#define BFILL 3
-#endif
-constexpr int FWD_SPREAD = 1024, FWD_FILL = FFILL;   // wavefronts: one, and four, to a vector unit
+constexpr int FWD_SPREAD = 1024, FWD_FILL = 6;   // wavefronts: one, and six, to a vector unit
 static int fwd_tiles(int dg) { return (dg + 63) / 64; }
 static int fwd_segment(const tgnn_seqs& q, int groups, int dg) { return scan_segment(q, (int64_t)groups * fwd_tiles(dg), FWD_SPREAD, FWD_FILL); }
 
 static int64_t fwd_bytes(const tgnn_seqs& q, int d, int n, int groups, ScanArgs* a, void* ws) {
   Take t{static_cast<char*>(ws)};
-  const int seg = fwd_segment(q, groups, d / groups);
-  if (seg != 0) {
-    float *st = t.floats(seg_total(q, seg) * d * n), *dl = t.floats(seg_total(q, seg) * d);
+  const int bits = fwd_segment(q, groups, d / groups);
+  if (bits != WHOLE) {
+    float *st = t.floats(seg_total(q, bits) * d * n), *dl = t.floats(seg_total(q, bits) * d);
     if (a) { a->seg_state = st; a->seg_delta = dl; }
   }
   return t.off;
@@ -721,7 +814,7 @@ static int launch_grid(int64_t n, unsigned* out) {
 }
 
 // Runs from 64 segments of the longest sequence on
-static bool chain_runs(const ScanArgs& a) { return std::min<int64_t>(a.q.max_len, scan_rows(a.q)) > 64 * (int64_t)a.seg; }
+static bool chain_runs(const ScanArgs& a) { return std::min<int64_t>(a.q.max_len, scan_rows(a.q)) > int64_t(64) << a.bits; }
 static int chain_grid(const ScanArgs& a, unsigned* out) {
   const int cols = chain_runs(a) ? 32 : 256;
   return launch_grid(a.q.n_seqs * (((int64_t)a.d * a.n + cols - 1) / cols), out);
@@ -740,18 +833,18 @@ template <class T, int NP, int MODE> static void launch_scan(const ScanArgs& a, 
 // The launches of a forward pass; MODE: SCAN_Y or SCAN_STATES
 template <int MODE> static int scan_forward(ScanArgs a, hipStream_t s, int dtype) {
   a.tiles = fwd_tiles(a.dg);
-  a.seg = fwd_segment(a.q, a.groups, a.dg);
-  a.items = a.seg ? seg_total(a.q, a.seg) : a.q.n_seqs;
+  a.bits = fwd_segment(a.q, a.groups, a.dg);
+  a.items = a.bits != WHOLE ? seg_total(a.q, a.bits) : a.q.n_seqs;
   const int64_t waves = a.items * a.groups * a.tiles;
   if (waves > INT_MAX) return set_error(TGNN_E_OUT_OF_RANGE, "%lld wavefronts", (long long)waves);
   const dim3 grid((unsigned)((waves + 3) / 4));
   unsigned chain = 0;
-  if (a.seg)
+  if (a.bits != WHOLE)
     if (int rc = chain_grid(a, &chain)) return rc;
   scan_shape(dtype, a.n, [&](auto t, auto np) {
     using T = decltype(t);
     constexpr int NP = decltype(np)::value;
-    if (a.seg) {
+    if (a.bits != WHOLE) {
       launch_scan<T, NP, SCAN_PART>(a, grid, s);
       launch_chain<false>(a, chain, s);
     }
@@ -761,18 +854,18 @@ template <int MODE> static int scan_forward(ScanArgs a, hipStream_t s, int dtype
   return TGNN_OK;
 }
 
-constexpr int BWD_SPREAD = 256, BWD_FILL = BFILL;   // workgroups: one, and three, to a compute unit
+constexpr int BWD_SPREAD = 256, BWD_FILL = 5;   // workgroups: one, and five, to a compute unit
 constexpr int BWD_WORKERS = 1024;   // at most as many partial sums of the weights' gradients
 
-struct BwdPlan { int np, tiles, seg, workers; int64_t items; };
+struct BwdPlan { int np, tiles, bits, workers; int64_t items; };
 static BwdPlan bwd_plan(const tgnn_seqs& q, int d, int n, int groups) {
   BwdPlan p;
   p.np = n <= 4 ? 1 : n <= 8 ? 2 : n <= 16 ? 4 : n <= 32 ? 8 : 16;
   const int cols = 16 * bwd_waves(p.np), dg = d / groups;
   p.tiles = (dg + cols - 1) / cols;
   const int64_t all = (int64_t)groups * p.tiles;
-  p.seg = scan_segment(q, all, BWD_SPREAD, BWD_FILL);
-  p.items = p.seg ? seg_total(q, p.seg) : q.n_seqs;
+  p.bits = scan_segment(q, all, BWD_SPREAD, BWD_FILL);
+  p.items = p.bits != WHOLE ? seg_total(q, p.bits) : q.n_seqs;
   p.workers = (int)std::max<int64_t>(1, std::min<int64_t>(p.items, std::min<int64_t>(BWD_WORKERS, 2 * BWD_SPREAD * BWD_FILL / all)));
   return p;
 }
@@ -780,13 +873,13 @@ static int64_t bwd_bytes(const tgnn_seqs& q, int d, int n, int groups, bool save
   const BwdPlan p = bwd_plan(q, d, n, groups);
   Take t{static_cast<char*>(ws)};
   if (!saved) {   // the states are formed here
-    float* sv = t.floats(seg_total(q, CHUNK) * d * n);
+    float* sv = t.floats(seg_total(q, CHUNK_BITS) * d * n);
     if (a) a->saved = fwd->saved = sv;
     const int64_t bytes = fwd_bytes(q, d, n, groups, fwd, ws ? static_cast<char*>(ws) + t.off : nullptr);
     t.off += bytes;
   }
-  if (p.seg) {
-    float *st = t.floats(seg_total(q, p.seg) * d * n), *dl = t.floats(seg_total(q, p.seg) * d);
+  if (p.bits != WHOLE) {
+    float *st = t.floats(seg_total(q, p.bits) * d * n), *dl = t.floats(seg_total(q, p.bits) * d);
     if (a) { a->seg_state = st; a->seg_delta = dl; }
   }
   float* part = t.floats((int64_t)p.workers * ((int64_t)d * n + 2 * d));
@@ -819,7 +912,7 @@ using namespace tgnn;
 
 extern "C" int64_t tgnn_selective_scan_saved_bytes(const tgnn_seqs* seqs, int32_t d, int32_t n_state) {
   if (int rc = check_sizes(seqs, d, n_state, 1)) return rc;
-  return seg_total(*seqs, CHUNK) * d * n_state * (int64_t)sizeof(float);
+  return seg_total(*seqs, CHUNK_BITS) * d * n_state * (int64_t)sizeof(float);
 }
 
 extern "C" int64_t tgnn_selective_scan_workspace_bytes(const tgnn_seqs* seqs, int32_t d, int32_t n_state, int32_t n_groups, int32_t backward,
@@ -874,14 +967,15 @@ extern "C" int32_t tgnn_selective_scan_step(const tgnn_scan* scan, int64_t n_row
   ScanArgs a = scan_args(nullptr, scan);
   a.y = y; a.ld_y = ld_y; a.state_out = state_out; a.items = n_rows;
   int bits = 0;
-  const int np = a.n >= 4 ? 4 : 1;
-  while ((np << bits) < a.n) ++bits;
+  while ((4 << bits) < a.n) ++bits;
+  const int tiles = (a.d + (256 >> bits) - 1) / (256 >> bits);
   unsigned grid;
-  if (int rc = launch_grid(((n_rows * a.d << bits) + 255) / 256, &grid)) return rc;
+  if (int rc = launch_grid((n_rows + 3) / 4 * tiles, &grid)) return rc;
   with_type(scan->dtype, [&](auto t) {
     using T = decltype(t);
-    if (np == 4) hipLaunchKernelGGL((scan_step_kernel<T, 4>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a, bits);
-    else hipLaunchKernelGGL((scan_step_kernel<T, 1>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a, bits);
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (bits >= 2) hipLaunchKernelGGL((scan_step_kernel<T, true>), dim3(grid), dim3(256), 0, s, a, bits, tiles);
+    else hipLaunchKernelGGL((scan_step_kernel<T, false>), dim3(grid), dim3(256), 0, s, a, bits, tiles);
   });
   TGNN_LAUNCH_CHECK();
   return TGNN_OK;
@@ -925,21 +1019,21 @@ extern "C" int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_sca
   a.dy = dy; a.ld_dy = ld_dy;
   a.dx = grads->dx; a.ddt = grads->ddt; a.dz = grads->dz; a.dB = grads->dB; a.dC = grads->dC;
   a.ld_dx = grads->ld_dx; a.ld_ddt = grads->ld_ddt; a.ld_dz = grads->ld_dz; a.ld_db = grads->ld_db; a.ld_dc = grads->ld_dc;
-  a.seg = plan.seg; a.items = plan.items;
+  a.bits = plan.bits; a.items = plan.items;
   const bool weights = grads->dA != nullptr || grads->dD != nullptr || grads->ddt_bias != nullptr;
   if (!weights) a.part = nullptr;
   if (seqs->n_seqs > 0) {
     unsigned chain = 0, back = 0, sum = 0;
     const int64_t waves = plan.items * a.groups * fwd_tiles(a.dg);
-    if (plan.seg) {
+    if (plan.bits != WHOLE) {
       if (int rc = chain_grid(a, &chain)) return rc;
       if (int rc = launch_grid(waves, &back)) return rc;
     }
-    if (int rc = launch_grid(seg_total(*seqs, CHUNK), &sum)) return rc;
+    if (int rc = launch_grid(seg_total(*seqs, SUM_BITS), &sum)) return rc;
     scan_shape(scan->dtype, a.n, [&](auto t, auto np) {
       using T = decltype(t);
       constexpr int NP = decltype(np)::value;
-      if (plan.seg) {
+      if (plan.bits != WHOLE) {
         a.tiles = fwd_tiles(a.dg);
         launch_scan<T, NP, SCAN_BACK_PART>(a, dim3((unsigned)((waves + 3) / 4)), s);
         launch_chain<true>(a, chain, s);

@@ -34,6 +34,10 @@ template <class T, int V> __device__ __forceinline__ void store_pack(T* p, const
   *reinterpret_cast<Pack<T, V>*>(p) = q;
 }
 
+// N values that are next to each other, at any address of one
+template <class T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Run { T v[N]; };
+template <int N> using FloatRun = Run<float, N>;
+
 inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 inline bool spans_overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);

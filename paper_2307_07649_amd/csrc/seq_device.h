@@ -35,67 +35,73 @@ __device__ __forceinline__ int64_t seq_row(const tgnn_seqs& q, const Seq& r, int
   return r.begin + (q.newest_first ? r.len - 1 - t : t);
 }
 
-// Segments of `seg` rows are numbered through all sequences: those of sequence s begin at seg_base(s) and are at most as many as lie
-// between that and seg_base(s + 1).  With row ranges the numbers come from the ranges themselves, begin / seg + s, which grows
-// by at least one and at least ceil(rows / seg) from a sequence to the next: no counting pass, and at most n_rows / seg + n_seqs
-// of them.
-__host__ __device__ __forceinline__ int64_t seg_per(const tgnn_seqs& q, int seg) {
-  return q.max_len > 0 ? ((int64_t)q.max_len + seg - 1) / seg : 1;
+// Segments of 2^bits rows are numbered through all sequences: those of sequence s begin at seg_base(s) and are at most as many as
+// lie between that and seg_base(s + 1).  With row ranges the numbers come from the ranges themselves, (begin >> bits) + s,
+// which grows by at least one and at least by the segments of its rows from a sequence to the next: no counting pass, and at
+// most (n_rows >> bits) + n_seqs of them (the host makes sure that they fit 31 bits).
+__host__ __device__ __forceinline__ int seg_per(const tgnn_seqs& q, int bits) {
+  return q.max_len > 0 ? (int)(((unsigned)q.max_len + (1u << bits) - 1) >> bits) : 1;
 }
-__device__ __forceinline__ int64_t seg_base(const tgnn_seqs& q, int s, int seg) {
-  if (q.indptr == nullptr) return (int64_t)s * seg_per(q, seg);
+__device__ __forceinline__ int seg_base(const tgnn_seqs& q, int s, int bits) {
+  if (q.indptr == nullptr) return s * seg_per(q, bits);
   const int64_t b = q.indptr[s];
-  return (b < 0 ? 0 : b > q.n_rows ? q.n_rows : b) / seg + s;
+  return (int)((b < 0 ? 0 : b > q.n_rows ? q.n_rows : b) >> bits) + s;
 }
-inline int64_t seg_total(const tgnn_seqs& q, int seg) {
-  return q.indptr == nullptr ? q.n_seqs * seg_per(q, seg) : q.n_rows / seg + q.n_seqs;
+inline int64_t seg_total(const tgnn_seqs& q, int bits) {
+  return q.indptr == nullptr ? (int64_t)q.n_seqs * seg_per(q, bits) : (q.n_rows >> bits) + q.n_seqs;
 }
-// The sequence of a segment, and which one of its own it is.
-__device__ __forceinline__ void seg_find(const tgnn_seqs& q, int64_t slot, int seg, int& s, int64_t& k) {
-  if (q.indptr == nullptr) {
-    const int64_t per = seg_per(q, seg);
-    s = (int)(slot / per);
-    k = slot - s * per;
-    return;
+// The sequence of a segment, the same one for all 64 lanes of a wavefront: the lanes look at 64 places at a time, so that 64
+// sequences take one load and 4,096 two.  (All lanes have to be there.)
+__device__ __forceinline__ int seg_find(const tgnn_seqs& q, int slot, int bits) {
+  if (q.indptr == nullptr) return (int)((unsigned)slot / (unsigned)seg_per(q, bits));
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = q.n_seqs;
+  while (n > 1) {
+    const int step = (n + 63) / 64, at = lo + min(lane * step, n - 1);
+    const bool before = lane * step < n && seg_base(q, at, bits) <= slot;
+    const int hits = __popcll(__ballot(before)), k = hits > 0 ? hits - 1 : 0;   // (the bases ascend: the hits come first)
+    lo += k * step;
+    n = min(step, n - k * step);
   }
-  int lo = 0, hi = q.n_seqs - 1;
-  while (lo < hi) {
-    const int mid = lo + (hi - lo + 1) / 2;
-    if (seg_base(q, mid, seg) <= slot) lo = mid; else hi = mid - 1;
-  }
-  s = lo;
-  k = slot - seg_base(q, lo, seg);
+  return __builtin_amdgcn_readfirstlane(lo);
 }
+// The same for a segment at or a little behind one whose sequence is known.
+__device__ __forceinline__ int seg_find_from(const tgnn_seqs& q, int slot, int bits, int s) {
+  if (q.indptr == nullptr) return (int)((unsigned)slot / (unsigned)seg_per(q, bits));
+  while (s + 1 < q.n_seqs && seg_base(q, s + 1, bits) <= slot) ++s;
+  return s;
+}
+// segments of a sequence of `len` events; an empty one has one
+__device__ __forceinline__ int seg_count(int len, int bits) { return len > 0 ? (int)(((unsigned)len + (1u << bits) - 1) >> bits) : 1; }
 
-// Work of one workgroup or wavefront: a segment of a sequence, or (seg == 0) a whole one.
+// Work of one workgroup or wavefront: a segment of a sequence, or a whole one.
+constexpr int MIN_SEG_BITS = 3;   // the shortest segments that anything is cut into
+constexpr int WHOLE = -1;   // for `bits`: sequences are not cut
 struct Piece {
   Seq r;
   int s;
-  int64_t slot;     // number of the segment (seg != 0)
+  int slot;         // number of the segment
   int t0, t1;       // its events
   bool last;        // the sequence ends here: final state and padding rows are this piece's
   bool none;        // a number without a segment
 };
-__device__ __forceinline__ Piece piece_at(const tgnn_seqs& q, int64_t item, int seg) {
+// The piece of number `item`, a segment of sequence s or the whole of it
+__device__ __forceinline__ Piece piece_of(const tgnn_seqs& q, int item, int bits, int s) {
   Piece p;
   p.slot = item;
-  int64_t k = 0;
-  if (seg == 0) p.s = (int)item;
-  else seg_find(q, item, seg, p.s, k);
-  p.r = seq_at(q, p.s);
-  if (seg == 0) {
-    p.t0 = 0;
-    p.t1 = p.r.len;
-    p.last = true;
-    p.none = false;
-    return p;
-  }
-  const int64_t need = p.r.len > 0 ? ((int64_t)p.r.len + seg - 1) / seg : 1;
-  p.none = k < 0 || k >= need;
-  p.t0 = p.none ? 0 : (int)(k * seg);
-  p.t1 = p.none ? 0 : (int)(k == need - 1 ? p.r.len : (k + 1) * seg);
+  p.s = s;
+  const int k = bits == WHOLE ? 0 : item - seg_base(q, s, bits);
+  p.r = seq_at(q, s);
+  const int need = bits == WHOLE ? 1 : seg_count(p.r.len, bits);
   p.last = k == need - 1;
+  p.none = k < 0 || k >= need;
+  p.t0 = p.none || bits == WHOLE ? 0 : k << bits;
+  p.t1 = p.none ? 0 : p.last ? p.r.len : (k + 1) << bits;
   return p;
+}
+// (for a number that is the same for the whole wavefront)
+__device__ __forceinline__ Piece piece_at(const tgnn_seqs& q, int item, int bits) {
+  return piece_of(q, item, bits, bits == WHOLE ? item : seg_find(q, item, bits));
 }
 
 int check_seqs(const tgnn_seqs* q);

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array
 
 import numpy as np
 import torch
@@ -184,33 +185,42 @@ def tgnn_memory_writeback_noalloc(st, src, dst, eid, t, s_src, s_dst, tau_src, t
 
 
 # ---- operators on sequences of events: plain functions, no context ----
+# Every function looks at its tensors once (types, shapes, strides, device) and hands pointers on; `dev` is the current GPU.
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 
-def _on_device(t, name):
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}: a tensor on the current GPU is needed")
+def _device_of(t):
+    return torch.cuda.current_device() if t.is_cuda else None
 
 
-def _rows(t, name, like=None, cols=None):
-    """(pointer, row distance) of a row array: two dimensions, values of a row next to each other."""
-    if t.dim() != 2 or t.dtype not in _DTYPES:
-        raise ValueError(f"{name}: a two-dimensional tensor of float32, bfloat16 or float16 is needed, not {tuple(t.shape)} {t.dtype}")
-    if like is not None and (t.dtype != like.dtype or t.shape[0] != like.shape[0] or t.shape[1] != (cols or like.shape[1])):
-        raise ValueError(f"{name}: {(like.shape[0], cols or like.shape[1])} {like.dtype} is needed, not {tuple(t.shape)} {t.dtype}")
-    if t.shape[0] > 0 and t.shape[1] > 1 and t.stride(1) != 1:
+def _elsewhere(t, name):
+    return ValueError(f"{name} is on {t.device}: a tensor on the current GPU is needed")
+
+
+def _rows(t, name, dev, dtype=None, shape=None):
+    """(pointer, row distance) of a row array: two dimensions, values of a row next to each other; dtype, shape: what it has to be."""
+    s = t.shape
+    if len(s) != 2 or t.dtype not in _DTYPES:
+        raise ValueError(f"{name}: a two-dimensional tensor of float32, bfloat16 or float16 is needed, not {tuple(s)} {t.dtype}")
+    if dtype is not None and (t.dtype != dtype or s != shape):
+        raise ValueError(f"{name}: {tuple(shape)} {dtype} is needed, not {tuple(s)} {t.dtype}")
+    ld, one = t.stride()
+    n, c = s
+    if one != 1 and c > 1 and n > 0:
         raise ValueError(f"{name}: the values of a row have to be contiguous")
-    _on_device(t, name)
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else t.shape[1])
+    if t.get_device() != dev:
+        raise _elsewhere(t, name)
+    return t.data_ptr(), (ld if n > 1 else c)
 
 
-def _floats(t, name, shape):
+def _floats(t, name, dev, shape):
     """Pointer of a contiguous float32 tensor of this shape, None for None."""
     if t is None:
         return None
-    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype != torch.float32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous float32 tensor {tuple(shape)} is needed, not {tuple(t.shape)} {t.dtype}")
-    _on_device(t, name)
+    if t.get_device() != dev:
+        raise _elsewhere(t, name)
     return t.data_ptr()
 
 
@@ -225,7 +235,7 @@ def _weight_grads(given, shapes, device):
         return [torch.empty(s, dtype=torch.float32, device=device) for s in shapes], 0
     if n != len(given):
         raise ValueError("the gradients of all weights are needed, or of none")
-    return list(given), 1
+    return given, 1
 
 
 class Seqs:
@@ -236,10 +246,11 @@ class Seqs:
     def __init__(self, n_rows, n_seqs, max_len, indptr=None, cnt=None, newest_first=False):
         for t, name, dtype, n in ((indptr, "indptr", torch.int64, n_seqs + 1), (cnt, "cnt", torch.int32, n_seqs)):
             if t is not None:
-                if t.dtype != dtype or tuple(t.shape) != (n,) or not t.is_contiguous():
+                if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
                     raise ValueError(f"{name}: a contiguous {dtype} tensor ({n},) is needed, not {tuple(t.shape)} {t.dtype}")
-                _on_device(t, name)
-        self.indptr, self.cnt, self.n_rows = indptr, cnt, n_rows
+                if t.get_device() != _device_of(t):
+                    raise _elsewhere(t, name)
+        self.indptr, self.cnt, self.n_rows, self.n_seqs = indptr, cnt, n_rows, n_seqs
         self.c = tgnn_seqs(None if indptr is None else indptr.data_ptr(), None if cnt is None else cnt.data_ptr(), n_rows, n_seqs,
                            max_len, 1 if newest_first else 0)
 
@@ -249,47 +260,57 @@ def _seq_rows(seqs, x):
         raise ValueError(f"x has {x.shape[0]} rows, the sequences {seqs.n_rows}")
 
 
-def _states(state_in, state_out, state_idx, n, shape, dtype):
+def _states(state_in, state_out, state_idx, dev, n, shape, dtype):
     """(state_in, state_out, state_idx, n_states) as the library takes them; n: sequences (or rows) of the call."""
-    given = [(t, name) for t, name in ((state_in, "state_in"), (state_out, "state_out")) if t is not None]
-    for t, name in given:
-        if t.dtype != dtype or tuple(t.shape[1:]) != shape or t.dim() != 3 or not t.is_contiguous() or t.shape[0] != given[0][0].shape[0]:
-            raise ValueError(f"{name}: a contiguous {dtype} tensor {('n_states',) + shape} is needed, not {tuple(t.shape)} {t.dtype}")
-        _on_device(t, name)
+    states, ptr = None, []
+    for t, name in ((state_in, "state_in"), (state_out, "state_out")):
+        if t is not None:
+            s = t.shape
+            if t.dtype != dtype or len(s) != 3 or s[1:] != shape or not t.is_contiguous() or (states is not None and s[0] != states):
+                raise ValueError(f"{name}: a contiguous {dtype} tensor {('n_states',) + shape} is needed, not {tuple(s)} {t.dtype}")
+            if t.get_device() != dev:
+                raise _elsewhere(t, name)
+            states = s[0]
+        ptr.append(None if t is None else t.data_ptr())
     if state_idx is not None:
-        if state_idx.dtype != torch.int32 or tuple(state_idx.shape) != (n,) or not state_idx.is_contiguous():
+        if state_idx.dtype != torch.int32 or state_idx.shape != (n,) or not state_idx.is_contiguous():
             raise ValueError(f"state_idx: a contiguous int32 tensor ({n},) is needed, not {tuple(state_idx.shape)} {state_idx.dtype}")
-        _on_device(state_idx, "state_idx")
-    elif given and given[0][0].shape[0] != n:
-        raise ValueError(f"{given[0][1]}: {n} states are needed without state_idx, not {given[0][0].shape[0]}")
-    ptr = [None if t is None else t.data_ptr() for t in (state_in, state_out, state_idx)]
-    return (*ptr, given[0][0].shape[0] if given else 0)
+        if state_idx.get_device() != dev:
+            raise _elsewhere(state_idx, "state_idx")
+        ptr.append(state_idx.data_ptr())
+    else:
+        if states is not None and states != n:
+            raise ValueError(f"{'state_in' if state_in is not None else 'state_out'}: {n} states are needed without state_idx, not {states}")
+        ptr.append(None)
+    return (*ptr, states or 0)
 
 
 def tgnn_causal_conv_fwd(seqs, x, weight, bias=None, silu=True, state_in=None, state_out=None, state_idx=None, out=None):
     """x [rows, d], float32, bfloat16 or float16; weight [d, width], bias [d] float32; states [n_states, width - 1, d] in x's type
     -> y (without `out` a new tensor, in which rows outside all slots hold nothing in particular)."""
     _seq_rows(seqs, x)
-    px, ldx = _rows(x, "x")
+    dev = _device_of(x)
+    px, ldx = _rows(x, "x", dev)
     d, w = x.shape[1], weight.shape[-1]
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    py, ldy = _rows(y, "out", like=x)
-    si, so, ix, ns = _states(state_in, state_out, state_idx, seqs.c.n_seqs, (w - 1, d), x.dtype)
-    _check(_lib.tgnn_causal_conv_fwd(seqs.c, _DTYPES[x.dtype], d, w, px, ldx, _floats(weight, "weight", (d, w)),
-                                     _floats(bias, "bias", (d,)), 1 if silu else 0, si, so, ix, ns, py, ldy, _stream()))
+    py, ldy = _rows(y, "out", dev, x.dtype, x.shape)
+    si, so, ix, ns = _states(state_in, state_out, state_idx, dev, seqs.n_seqs, (w - 1, d), x.dtype)
+    _check(_lib.tgnn_causal_conv_fwd(seqs.c, _DTYPES[x.dtype], d, w, px, ldx, _floats(weight, "weight", dev, (d, w)),
+                                     _floats(bias, "bias", dev, (d,)), 1 if silu else 0, si, so, ix, ns, py, ldy, _stream()))
     return y
 
 
 def tgnn_causal_conv_step(x, weight, bias=None, silu=True, state_in=None, state_out=None, state_idx=None, out=None):
     """One event per row of x; state_out may be state_in -> y."""
-    px, ldx = _rows(x, "x")
+    dev = _device_of(x)
+    px, ldx = _rows(x, "x", dev)
     n, d = x.shape
     w = weight.shape[-1]
     y = torch.empty(n, d, dtype=x.dtype, device=x.device) if out is None else out
-    py, ldy = _rows(y, "out", like=x)
-    si, so, ix, ns = _states(state_in, state_out, state_idx, n, (w - 1, d), x.dtype)
-    _check(_lib.tgnn_causal_conv_step(_DTYPES[x.dtype], n, d, w, px, ldx, _floats(weight, "weight", (d, w)), _floats(bias, "bias", (d,)),
-                                      1 if silu else 0, si, so, ix, ns, py, ldy, _stream()))
+    py, ldy = _rows(y, "out", dev, x.dtype, x.shape)
+    si, so, ix, ns = _states(state_in, state_out, state_idx, dev, n, (w - 1, d), x.dtype)
+    _check(_lib.tgnn_causal_conv_step(_DTYPES[x.dtype], n, d, w, px, ldx, _floats(weight, "weight", dev, (d, w)),
+                                      _floats(bias, "bias", dev, (d,)), 1 if silu else 0, si, so, ix, ns, py, ldy, _stream()))
     return y
 
 
@@ -297,34 +318,37 @@ def tgnn_causal_conv_bwd(seqs, dy, x, weight, bias=None, silu=True, state_in=Non
                          out=None):
     """-> dx, d_weight, d_bias.  Given d_weight and d_bias are added to; without them new ones are written."""
     _seq_rows(seqs, x)
-    px, ldx = _rows(x, "x")
-    pdy, lddy = _rows(dy, "dy", like=x)
+    dev = _device_of(x)
+    px, ldx = _rows(x, "x", dev)
+    pdy, lddy = _rows(dy, "dy", dev, x.dtype, x.shape)
     d, w = x.shape[1], weight.shape[-1]
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    pdx, lddx = _rows(dx, "out", like=x)
+    pdx, lddx = _rows(dx, "out", dev, x.dtype, x.shape)
     (dw, db), add = _weight_grads((d_weight, d_bias), ((d, w), (d,)), x.device)
-    si, _, ix, ns = _states(state_in, None, state_idx, seqs.c.n_seqs, (w - 1, d), x.dtype)
+    si, _, ix, ns = _states(state_in, None, state_idx, dev, seqs.n_seqs, (w - 1, d), x.dtype)
     ws = _workspace(_lib.tgnn_causal_conv_workspace_bytes(d, w), x.device)
-    _check(_lib.tgnn_causal_conv_bwd(seqs.c, _DTYPES[x.dtype], d, w, pdy, lddy, px, ldx, _floats(weight, "weight", (d, w)),
-                                     _floats(bias, "bias", (d,)), 1 if silu else 0, si, ix, ns, pdx, lddx, _floats(dw, "d_weight", (d, w)),
-                                     _floats(db, "d_bias", (d,)), add, ws.data_ptr(), ws.numel(), _stream()))
+    _check(_lib.tgnn_causal_conv_bwd(seqs.c, _DTYPES[x.dtype], d, w, pdy, lddy, px, ldx, _floats(weight, "weight", dev, (d, w)),
+                                     _floats(bias, "bias", dev, (d,)), 1 if silu else 0, si, ix, ns, pdx, lddx,
+                                     _floats(dw, "d_weight", dev, (d, w)), _floats(db, "d_bias", dev, (d,)), add, ws.data_ptr(),
+                                     ws.numel(), _stream()))
     return dx, dw, db
 
 
-def _scan_args(x, dt, A, B, Cm, D, z, dt_bias, softplus, states):
-    px, ldx = _rows(x, "x")
+def _scan_args(x, dt, A, B, Cm, D, z, dt_bias, softplus, dev, states):
+    px, ldx = _rows(x, "x", dev)
+    dtype, shape, bc = x.dtype, x.shape, B.shape
     if A.dim() != 2:
         raise ValueError(f"A: a float32 tensor (d, n_state) is needed, not {tuple(A.shape)} {A.dtype}")
     d, n = A.shape
-    if x.shape[1] != d or n == 0 or B.dim() != 2 or B.shape[1] % n != 0 or B.shape[1] == 0:
-        raise ValueError(f"x {tuple(x.shape)}, A {tuple(A.shape)} and B {tuple(B.shape)} do not belong together")
-    pdt, lddt = _rows(dt, "dt", like=x)
-    pb, ldb = _rows(B, "B", like=x, cols=B.shape[1])
-    pc, ldc = _rows(Cm, "C", like=x, cols=B.shape[1])
-    pz, ldz = (None, 0) if z is None else _rows(z, "z", like=x)
+    if shape[1] != d or n == 0 or len(bc) != 2 or bc[0] != shape[0] or bc[1] % n != 0 or bc[1] == 0:
+        raise ValueError(f"x {tuple(shape)}, A {tuple(A.shape)} and B {tuple(bc)} do not belong together")
+    pdt, lddt = _rows(dt, "dt", dev, dtype, shape)
+    pb, ldb = _rows(B, "B", dev, dtype, bc)
+    pc, ldc = _rows(Cm, "C", dev, dtype, bc)
+    pz, ldz = (None, 0) if z is None else _rows(z, "z", dev, dtype, shape)
     si, _, ix, ns = states
-    return tgnn_scan(_DTYPES[x.dtype], d, n, B.shape[1] // n, 1 if softplus else 0, ns, px, pdt, pb, pc, pz, ldx, lddt, ldb, ldc, ldz,
-                     _floats(A, "A", (d, n)), _floats(D, "D", (d,)), _floats(dt_bias, "dt_bias", (d,)), si, ix)
+    return tgnn_scan(_DTYPES[dtype], d, n, bc[1] // n, 1 if softplus else 0, ns, px, pdt, pb, pc, pz, ldx, lddt, ldb, ldc, ldz,
+                     _floats(A, "A", dev, (d, n)), _floats(D, "D", dev, (d,)), _floats(dt_bias, "dt_bias", dev, (d,)), si, ix)
 
 
 def _bytes(n):
@@ -338,10 +362,10 @@ def selective_scan_saved(seqs, A):
     return torch.empty(_bytes(_lib.tgnn_selective_scan_saved_bytes(seqs.c, *A.shape)) // 4, dtype=torch.float32, device=A.device)
 
 
-def _saved(saved):
+def _saved(saved, dev):
     if saved is None:
         return None, 0
-    return _floats(saved, "saved", saved.shape), saved.numel() * 4
+    return _floats(saved, "saved", dev, saved.shape), saved.numel() * 4
 
 
 def tgnn_selective_scan_fwd(seqs, x, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, state_in=None, state_out=None,
@@ -350,11 +374,12 @@ def tgnn_selective_scan_fwd(seqs, x, dt, A, B, C, D=None, z=None, dt_bias=None, 
     states [n_states, d, n_state] float32; saved: selective_scan_saved(...) -> y (without `out` a new tensor, in which rows outside all
     slots hold nothing in particular)."""
     _seq_rows(seqs, x)
-    states = _states(state_in, state_out, state_idx, seqs.c.n_seqs, tuple(A.shape), torch.float32)
-    a = _scan_args(x, dt, A, B, C, D, z, dt_bias, softplus, states)
+    dev = _device_of(x)
+    states = _states(state_in, state_out, state_idx, dev, seqs.n_seqs, tuple(A.shape), torch.float32)
+    a = _scan_args(x, dt, A, B, C, D, z, dt_bias, softplus, dev, states)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    py, ldy = _rows(y, "out", like=x)
-    ps, ns = _saved(saved)
+    py, ldy = _rows(y, "out", dev, x.dtype, x.shape)
+    ps, ns = _saved(saved, dev)
     need = _bytes(_lib.tgnn_selective_scan_workspace_bytes(seqs.c, a.d, a.n_state, a.n_groups, 0, 0))
     ws = _workspace(need, x.device) if need else None
     _check(_lib.tgnn_selective_scan_fwd(seqs.c, a, py, ldy, states[1], ps, ns, ws.data_ptr() if need else None, need, _stream()))
@@ -364,10 +389,11 @@ def tgnn_selective_scan_fwd(seqs, x, dt, A, B, C, D=None, z=None, dt_bias=None, 
 def tgnn_selective_scan_step(x, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=True, state_in=None, state_out=None,
                              state_idx=None, out=None):
     """One event per row; state_out may be state_in -> y."""
-    states = _states(state_in, state_out, state_idx, x.shape[0], tuple(A.shape), torch.float32)
-    a = _scan_args(x, dt, A, B, C, D, z, dt_bias, softplus, states)
+    dev = _device_of(x)
+    states = _states(state_in, state_out, state_idx, dev, x.shape[0], tuple(A.shape), torch.float32)
+    a = _scan_args(x, dt, A, B, C, D, z, dt_bias, softplus, dev, states)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    py, ldy = _rows(y, "out", like=x)
+    py, ldy = _rows(y, "out", dev, x.dtype, x.shape)
     _check(_lib.tgnn_selective_scan_step(a, x.shape[0], py, ldy, states[1], _stream()))
     return y
 
@@ -377,22 +403,22 @@ def tgnn_selective_scan_bwd(seqs, dy, x, dt, A, B, C, D=None, z=None, dt_bias=No
     """-> dict of dx, ddt, dB, dC, dA and, with z, D, dt_bias given, dz, dD, ddt_bias.  Given gradients of the weights (of all
     that there are) are added to; without them new ones are written.  out: a dict of the row arrays to write (dx, ddt, dB, dC, dz)."""
     _seq_rows(seqs, x)
-    states = _states(state_in, None, state_idx, seqs.c.n_seqs, tuple(A.shape), torch.float32)
-    a = _scan_args(x, dt, A, B, C, D, z, dt_bias, softplus, states)
-    pdy, lddy = _rows(dy, "dy", like=x)
-    names = ["dA"] + ["dD"] * (D is not None) + ["ddt_bias"] * (dt_bias is not None)
-    given = dict(dA=dA, dD=dD, ddt_bias=ddt_bias)
-    if any(g is not None and n not in names for n, g in given.items()):
+    dev = _device_of(x)
+    states = _states(state_in, None, state_idx, dev, seqs.n_seqs, tuple(A.shape), torch.float32)
+    a = _scan_args(x, dt, A, B, C, D, z, dt_bias, softplus, dev, states)
+    dtype, shape, bc = x.dtype, x.shape, B.shape
+    pdy, lddy = _rows(dy, "dy", dev, dtype, shape)
+    weights = [(n, g) for n, g, v in (("dA", dA, A), ("dD", dD, D), ("ddt_bias", ddt_bias, dt_bias)) if v is not None]
+    if (dD is not None and D is None) or (ddt_bias is not None and dt_bias is None):
         raise ValueError("a gradient of a weight that there is none of")
-    w, add = _weight_grads([given[n] for n in names], [tuple(A.shape) if n == "dA" else (a.d,) for n in names], x.device)
-    like = dict(dx=x, ddt=x, dB=B, dC=B, dz=z)
-    g = {n: torch.empty(v.shape, dtype=x.dtype, device=x.device) if out is None else out[n] for n, v in like.items() if v is not None}
-    rows = [(None, 0) if v is None else _rows(g[n], n, like=v) for n, v in like.items()]
-    g.update(zip(names, w))
-    c = tgnn_scan_grads(*[r[0] for r in rows], *[r[1] for r in rows],
-                        _floats(g["dA"], "dA", tuple(A.shape)), _floats(g.get("dD"), "dD", (a.d,)),
-                        _floats(g.get("ddt_bias"), "ddt_bias", (a.d,)))
-    ps, ns = _saved(saved)
+    w, add = _weight_grads([v for _, v in weights], [A.shape if n == "dA" else (a.d,) for n, _ in weights], x.device)
+    like = (("dx", shape), ("ddt", shape), ("dB", bc), ("dC", bc)) + ((("dz", shape),) if z is not None else ())
+    g = {n: torch.empty(s, dtype=dtype, device=x.device) if out is None else out[n] for n, s in like}
+    rows = [_rows(g[n], n, dev, dtype, s) for n, s in like] + ([] if z is not None else [(None, 0)])
+    g.update((n, v) for (n, _), v in zip(weights, w))
+    c = tgnn_scan_grads(*[r[0] for r in rows], *[r[1] for r in rows], _floats(g["dA"], "dA", dev, A.shape),
+                        _floats(g.get("dD"), "dD", dev, (a.d,)), _floats(g.get("ddt_bias"), "ddt_bias", dev, (a.d,)))
+    ps, ns = _saved(saved, dev)
     need = _bytes(_lib.tgnn_selective_scan_workspace_bytes(seqs.c, a.d, a.n_state, a.n_groups, 1, 0 if saved is None else 1))
     ws = _workspace(need, x.device)
     _check(_lib.tgnn_selective_scan_bwd(seqs.c, a, pdy, lddy, ps, ns, c, add, ws.data_ptr(), need, _stream()))
@@ -401,64 +427,75 @@ def tgnn_selective_scan_bwd(seqs, dy, x, dt, A, B, C, D=None, z=None, dt_bias=No
 
 def tgnn_layer_norm_fwd(x, weight=None, bias=None, eps=1e-5, out=None):
     """x [rows, cols], float32, bfloat16 or float16; weight, bias: float32 [cols] or None -> y, mean, rstd."""
-    px, ldx = _rows(x, "x")
+    dev = _device_of(x)
+    px, ldx = _rows(x, "x", dev)
     n, c = x.shape
     y = torch.empty(n, c, dtype=x.dtype, device=x.device) if out is None else out
-    py, ldy = _rows(y, "out", like=x)
+    py, ldy = _rows(y, "out", dev, x.dtype, x.shape)
     mean, rstd = torch.empty(2, n, dtype=torch.float32, device=x.device).unbind(0)
-    _check(_lib.tgnn_layer_norm_fwd(_DTYPES[x.dtype], n, c, px, ldx, _floats(weight, "weight", (c,)), _floats(bias, "bias", (c,)), eps,
-                                    py, ldy, mean.data_ptr(), rstd.data_ptr(), _stream()))
+    _check(_lib.tgnn_layer_norm_fwd(_DTYPES[x.dtype], n, c, px, ldx, _floats(weight, "weight", dev, (c,)),
+                                    _floats(bias, "bias", dev, (c,)), eps, py, ldy, mean.data_ptr(), rstd.data_ptr(), _stream()))
     return y, mean, rstd
 
 
 def tgnn_layer_norm_bwd(dy, x, mean, rstd, weight=None, d_weight=None, d_bias=None, out=None):
     """-> dx, d_weight, d_bias.  Given d_weight and d_bias are added to; without them new ones are written."""
-    px, ldx = _rows(x, "x")
-    pdy, lddy = _rows(dy, "dy", like=x)
+    dev = _device_of(x)
+    px, ldx = _rows(x, "x", dev)
+    pdy, lddy = _rows(dy, "dy", dev, x.dtype, x.shape)
     n, c = x.shape
     dx = torch.empty(n, c, dtype=x.dtype, device=x.device) if out is None else out
-    pdx, lddx = _rows(dx, "out", like=x)
+    pdx, lddx = _rows(dx, "out", dev, x.dtype, x.shape)
     (dw, db), add = _weight_grads((d_weight, d_bias), ((c,), (c,)), x.device)
     ws = _workspace(_lib.tgnn_layer_norm_workspace_bytes(n, c), x.device)
-    _check(_lib.tgnn_layer_norm_bwd(_DTYPES[x.dtype], n, c, pdy, lddy, px, ldx, _floats(mean, "mean", (n,)), _floats(rstd, "rstd", (n,)),
-                                    _floats(weight, "weight", (c,)), pdx, lddx, _floats(dw, "d_weight", (c,)),
-                                    _floats(db, "d_bias", (c,)), add, ws.data_ptr(), ws.numel(), _stream()))
+    _check(_lib.tgnn_layer_norm_bwd(_DTYPES[x.dtype], n, c, pdy, lddy, px, ldx, _floats(mean, "mean", dev, (n,)),
+                                    _floats(rstd, "rstd", dev, (n,)), _floats(weight, "weight", dev, (c,)), pdx, lddx,
+                                    _floats(dw, "d_weight", dev, (c,)), _floats(db, "d_bias", dev, (c,)), add, ws.data_ptr(),
+                                    ws.numel(), _stream()))
     return dx, dw, db
 
 
-def _tensor_list(tensors, name):
-    """Host arrays (pointers, numbers of elements, types) of a list of contiguous tensors or of a Params set."""
-    ts = list(tensors.t.values()) if isinstance(tensors, Params) else list(tensors)
+def _tensor_list(tensors, name, like=None):
+    """Host arrays (pointers, numbers of elements, types) of a list of contiguous tensors or of a Params set, and the first
+    tensor's device; like: the numbers and types that they have to have."""
+    ts = tensors.t.values() if isinstance(tensors, Params) else tensors
+    ptr, numel, kind, device, dev = array("Q"), array("q"), array("i"), None, None
     for t in ts:
-        if t.dtype not in _DTYPES or not t.is_contiguous():
+        k = _DTYPES.get(t.dtype)
+        if k is None or not t.is_contiguous():
             raise ValueError(f"{name}: contiguous tensors of float32, bfloat16 or float16 are needed, not {tuple(t.shape)} {t.dtype}")
-        _on_device(t, name)
-    n = len(ts)
-    return ts, (_P * n)(*[t.data_ptr() or None for t in ts]), (_L * n)(*[t.numel() for t in ts]), (_I * n)(*[_DTYPES[t.dtype] for t in ts])
+        if dev is None:
+            device, dev = t.device, _device_of(t)
+        if t.get_device() != dev:
+            raise _elsewhere(t, name)
+        ptr.append(t.data_ptr())
+        numel.append(t.numel())
+        kind.append(k)
+    if like is not None and (numel != like[1] or kind != like[2]):
+        raise ValueError(f"{name}: tensors of the gradients' sizes and types are needed")
+    return ptr, numel, kind, device
 
 
 def tgnn_grad_norm(grads, out_norm=None):
     """grads: a list of tensors, or a Params set -> the square root of the sum of all their squares, float32 [1]."""
-    ts, ptr, numel, dtype = _tensor_list(grads, "grads")
-    norm = torch.empty(1, dtype=torch.float32, device=ts[0].device if ts else "cuda") if out_norm is None else out_norm
-    ws = _workspace(_lib.tgnn_clip_workspace_bytes(len(ts)), norm.device)
-    _check(_lib.tgnn_grad_norm(len(ts), ptr, numel, dtype, _floats(norm, "out_norm", (1,)), ws.data_ptr(), ws.numel(), _stream()))
+    ptr, numel, kind, device = _tensor_list(grads, "grads")
+    norm = torch.empty(1, dtype=torch.float32, device=device or "cuda") if out_norm is None else out_norm
+    ws = _workspace(_lib.tgnn_clip_workspace_bytes(len(ptr)), norm.device)
+    _check(_lib.tgnn_grad_norm(len(ptr), ptr.buffer_info()[0], numel.buffer_info()[0], kind.buffer_info()[0],
+                               _floats(norm, "out_norm", _device_of(norm), (1,)), ws.data_ptr(), ws.numel(), _stream()))
     return norm
 
 
 def tgnn_clip_grads(grads, max_norm, out=None, out_norm=None):
     """Scales the gradients to a global norm of at most max_norm, in place or into `out` (tensors of the same sizes and types)
     -> their norm before, float32 [1]."""
-    ts, ptr, numel, dtype = _tensor_list(grads, "grads")
-    to = None
-    if out is not None:
-        os_, to, n_out, dt_out = _tensor_list(out, "out")
-        if len(os_) != len(ts) or list(n_out) != list(numel) or list(dt_out) != list(dtype):
-            raise ValueError("out: tensors of the gradients' sizes and types are needed")
-    norm = torch.empty(1, dtype=torch.float32, device=ts[0].device if ts else "cuda") if out_norm is None else out_norm
-    ws = _workspace(_lib.tgnn_clip_workspace_bytes(len(ts)), norm.device)
-    _check(_lib.tgnn_clip_grads(len(ts), ptr, numel, dtype, max_norm, to, _floats(norm, "out_norm", (1,)), ws.data_ptr(), ws.numel(),
-                                _stream()))
+    ptr, numel, kind, device = given = _tensor_list(grads, "grads")
+    to = None if out is None else _tensor_list(out, "out", given)[0]
+    norm = torch.empty(1, dtype=torch.float32, device=device or "cuda") if out_norm is None else out_norm
+    ws = _workspace(_lib.tgnn_clip_workspace_bytes(len(ptr)), norm.device)
+    _check(_lib.tgnn_clip_grads(len(ptr), ptr.buffer_info()[0], numel.buffer_info()[0], kind.buffer_info()[0], max_norm,
+                                None if to is None else to.buffer_info()[0], _floats(norm, "out_norm", _device_of(norm), (1,)),
+                                ws.data_ptr(), ws.numel(), _stream()))
     return norm
 
 

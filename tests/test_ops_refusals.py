@@ -107,7 +107,8 @@ CONV_BWD = (["seqs", "dtype", "d", "width", "dy", "ld_dy", "x", "ld_x", "weight"
 
 SEQS_BAD = [(dict(n_seqs=-1), INVALID, "negative"), (dict(max_len=-1), INVALID, "negative"), (dict(n_rows=-1), INVALID, "negative"),
             (dict(newest_first=2), INVALID, "newest_first"), (dict(indptr=P + 4), MISALIGNED, "indptr"), (dict(cnt=P + 2), MISALIGNED, "cnt"),
-            (dict(max_len=11), RANGE, "do not fit"), (dict(n_rows=1 << 34, indptr=P), RANGE, "rows")]
+            (dict(max_len=11), RANGE, "do not fit"), (dict(n_rows=1 << 33, indptr=P), RANGE, "rows"),
+            (dict(n_rows=(1 << 33) - 1, n_seqs=(1 << 31) - 1, indptr=P), RANGE, "sequences")]
 
 
 @pytest.mark.parametrize("seqs,code,word", SEQS_BAD)
