@@ -34,43 +34,37 @@ struct ConvArgs {
 
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
 
-// Taps of V columns; W == CONV_ANY: any number of them up to that, in the places behind.  (V * W values next to each other: as
-// vector loads, for which four bytes are aligned enough.)
-template <int V, int W> __device__ __forceinline__ void conv_taps(const ConvArgs& a, int c, float (&w)[W][V], float (&b)[V]) {
+// Taps of V columns, `left` of which there are; W == CONV_ANY: any number of them up to that, in the places behind.  (V * W values
+// next to each other: as vector loads, for which four bytes are aligned enough.)
+template <int V, int W> __device__ __forceinline__ void conv_taps(const ConvArgs& a, int c, int left, float (&w)[W][V], float (&b)[V]) {
   if constexpr (W != CONV_ANY) {
-    const FloatRun<V * W> r = *reinterpret_cast<const FloatRun<V * W>*>(a.w + (int64_t)c * W);
+    float r[V * W];
+    take_floats<V * W>(a.w + (int64_t)c * W, left * W, 0.0f, r);
 #pragma unroll
     for (int i = 0; i < V; ++i)
 #pragma unroll
-      for (int j = 0; j < W; ++j) w[j][i] = r.v[i * W + j];
+      for (int j = 0; j < W; ++j) w[j][i] = r[i * W + j];
   } else {
 #pragma unroll
     for (int i = 0; i < V; ++i)
 #pragma unroll
       for (int j = 0; j < W; ++j) {
         const int k = j - (W - a.width);
-        w[j][i] = k >= 0 ? a.w[(int64_t)(c + i) * a.width + k] : 0.0f;
+        w[j][i] = k >= 0 && i < left ? a.w[(int64_t)(c + i) * a.width + k] : 0.0f;
       }
   }
-  if (a.bias) {
-    const FloatRun<V> r = *reinterpret_cast<const FloatRun<V>*>(a.bias + c);
-#pragma unroll
-    for (int i = 0; i < V; ++i) b[i] = r.v[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) b[i] = 0.0f;
-  }
+  take_floats<V>(a.bias ? a.bias + c : nullptr, left, 0.0f, b);
 }
 // the input at place t of the sequence: a row, a row of the state, or zero
-template <class T, int V> __device__ __forceinline__ void conv_input(const ConvArgs& a, const Seq& r, int64_t state, int t, int c, float (&v)[V]) {
-  if (t >= 0) {
-    load_pack<T, V>(static_cast<const T*>(a.x) + seq_row(a.q, r, t) * a.ld_x + c, v);
-  } else if (state >= 0 && a.state_in != nullptr) {
-    load_pack<T, V>(static_cast<const T*>(a.state_in) + (state * (a.width - 1) + (a.width - 1) + t) * a.d + c, v);
-  } else {
+template <class T, int V, bool ANY>
+__device__ __forceinline__ void conv_input(const ConvArgs& a, const Seq& r, int64_t state, int t, int c, float (&v)[V]) {
+  const T* p = nullptr;
+  if (t >= 0) p = static_cast<const T*>(a.x) + seq_row(a.q, r, t) * a.ld_x + c;
+  else if (state >= 0 && a.state_in != nullptr) p = static_cast<const T*>(a.state_in) + (state * (a.width - 1) + (a.width - 1) + t) * a.d + c;
+  if (p != nullptr) unpack(take<T, V, ANY>(p, a.d - c), v);
+  else
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = 0.0f;
-  }
 }
 template <int V, int W> __device__ __forceinline__ void conv_sum(const ConvArgs& a, const float (&win)[W][V], const float (&w)[W][V],
                                                                 const float (&b)[V], float (&pre)[V]) {
@@ -95,8 +89,8 @@ __device__ __forceinline__ int64_t state_of(const int32_t* idx, int n_states, in
   return i >= 0 && i < n_states ? i : -1;
 }
 
-// WIDE: a wavefront's threads are all at one segment.
-template <class T, int V, int W, bool WIDE>
+// WIDE: a wavefront's threads are all at one segment.  ANY: rows at any address, of any number of columns.
+template <class T, int V, int W, bool WIDE, bool ANY>
 __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
   const int per_y = 256 / a.per_x, col_tiles = (a.d + a.per_x * V - 1) / (a.per_x * V);
   const int c = ((int)(blockIdx.x % col_tiles) * a.per_x + (int)threadIdx.x % a.per_x) * V;
@@ -108,7 +102,7 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
   if (p.none) return;
   const int64_t state = state_of(a.state_idx, a.n_states, p.s);
   float w[W][V], b[V], win[W][V];
-  conv_taps<V, W>(a, c, w, b);
+  conv_taps<V, W>(a, c, a.d - c, w, b);
 #pragma unroll
   for (int j = 0; j < W; ++j)
 #pragma unroll
@@ -117,7 +111,7 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
   for (int j = 0; j + 1 < W; ++j)
     if (j + 1 < a.width) {   // the places t0 - (width - 1) .. t0 - 1
       float v[V];
-      conv_input<T, V>(a, p.r, state, p.t0 - (a.width - 1) + j, c, v);
+      conv_input<T, V, ANY>(a, p.r, state, p.t0 - (a.width - 1) + j, c, v);
       shift_in<V, W>(win, v);
     }
   // rows are asked for AHEAD before their use
@@ -127,7 +121,7 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
   Pack<T, V> next[AHEAD];
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u)
-    if (p.t0 + u < p.t1) next[u] = *reinterpret_cast<const Pack<T, V>*>(x + u * step * a.ld_x);
+    if (p.t0 + u < p.t1) next[u] = take<T, V, ANY>(x + u * step * a.ld_x, a.d - c);
   const bool silu = a.silu != 0;
   auto row = [&](int u) {
     float v[V], pre[V];
@@ -137,7 +131,7 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
     conv_sum<V, W>(a, win, w, b, pre);
 #pragma unroll
     for (int i = 0; i < V; ++i) pre[i] *= silu ? sigmoid(pre[i]) : 1.0f;
-    store_pack<T, V>(y + u * step * a.ld_y, pre);
+    put<T, V, ANY>(y + u * step * a.ld_y, pre, a.d - c);
   };
   int t = p.t0;
   for (; t + AHEAD <= p.t1; t += AHEAD) {   // whole groups
@@ -145,7 +139,7 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
     for (int u = 0; u < AHEAD; ++u) {
       row(u);
       const int ahead = min(u + AHEAD, p.t1 - 1 - t);   // (past the end: a row that is there)
-      next[u] = *reinterpret_cast<const Pack<T, V>*>(x + ahead * step * a.ld_x);
+      next[u] = take<T, V, ANY>(x + ahead * step * a.ld_x, a.d - c);
     }
     x += AHEAD * step * a.ld_x;
     y += AHEAD * step * a.ld_y;
@@ -155,18 +149,18 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
     if (t + u < p.t1) row(u);
   if (!p.last) return;
   float zero[V] = {};
-  for (int t = p.r.len; t < p.r.slot; ++t) store_pack<T, V>(static_cast<T*>(a.y) + (p.r.begin + t) * a.ld_y + c, zero);
+  for (int t = p.r.len; t < p.r.slot; ++t) put<T, V, ANY>(static_cast<T*>(a.y) + (p.r.begin + t) * a.ld_y + c, zero, a.d - c);
   if (state >= 0 && a.state_out != nullptr)
 #pragma unroll
     for (int j = 1; j < W; ++j)
       if (j >= W - (a.width - 1))
-        store_pack<T, V>(static_cast<T*>(a.state_out) + (state * (a.width - 1) + j - (W - (a.width - 1))) * a.d + c, win[j]);
+        put<T, V, ANY>(static_cast<T*>(a.state_out) + (state * (a.width - 1) + j - (W - (a.width - 1))) * a.d + c, win[j], a.d - c);
 }
 
 // One event of each of `items` nodes.
-template <class T, int V, int W>
+template <class T, int V, int W, bool ANY>
 __global__ __launch_bounds__(256) void conv_step_kernel(ConvArgs a) {
-  const int packs = a.d / V;
+  const int packs = (a.d + V - 1) / V;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= a.items * packs) return;
   const int64_t row = i / packs;
@@ -181,24 +175,24 @@ __global__ __launch_bounds__(256) void conv_step_kernel(ConvArgs a) {
   for (int j = 0; j + 1 < W; ++j) {
     const int k = j - (W - a.width);
     if (k >= 0 && state >= 0 && a.state_in != nullptr)
-      load_pack<T, V>(static_cast<const T*>(a.state_in) + (state * (a.width - 1) + k) * a.d + c, win[j]);
+      unpack(take<T, V, ANY>(static_cast<const T*>(a.state_in) + (state * (a.width - 1) + k) * a.d + c, a.d - c), win[j]);
   }
-  load_pack<T, V>(static_cast<const T*>(a.x) + row * a.ld_x + c, win[W - 1]);
-  conv_taps<V, W>(a, c, w, b);
+  unpack(take<T, V, ANY>(static_cast<const T*>(a.x) + row * a.ld_x + c, a.d - c), win[W - 1]);
+  conv_taps<V, W>(a, c, a.d - c, w, b);
   conv_sum<V, W>(a, win, w, b, pre);
   if (a.silu)
 #pragma unroll
     for (int k = 0; k < V; ++k) pre[k] *= sigmoid(pre[k]);
-  store_pack<T, V>(static_cast<T*>(a.y) + row * a.ld_y + c, pre);
+  put<T, V, ANY>(static_cast<T*>(a.y) + row * a.ld_y + c, pre, a.d - c);
   if (state >= 0 && a.state_out != nullptr)
 #pragma unroll
     for (int j = 1; j < W; ++j) {
       const int k = j - 1 - (W - a.width);
-      if (k >= 0) store_pack<T, V>(static_cast<T*>(a.state_out) + (state * (a.width - 1) + k) * a.d + c, win[j]);
+      if (k >= 0) put<T, V, ANY>(static_cast<T*>(a.state_out) + (state * (a.width - 1) + k) * a.d + c, win[j], a.d - c);
     }
 }
 
-template <class T, int V, int W, bool WIDE>
+template <class T, int V, int W, bool WIDE, bool ANY>
 __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
   __shared__ float acc[256 * V];
   const int per_y = 256 / a.per_x, col_tiles = (a.d + a.per_x * V - 1) / (a.per_x * V);
@@ -213,7 +207,7 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
 #pragma unroll
     for (int j = 0; j < W; ++j) w[j][i] = dw[j][i] = 0.0f;
   }
-  if (on) conv_taps<V, W>(a, c, w, b);
+  if (on) conv_taps<V, W>(a, c, a.d - c, w, b);
   const int halo = a.width - 1;
   for (int64_t item0 = (int64_t)worker * per_y; item0 < a.items; item0 += (int64_t)workers * per_y) {
     const int s0 = seg_find(a.q, (int)item0, a.bits), item = (int)item0 + ty;
@@ -231,7 +225,7 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
     for (int j = 0; j + 1 < W; ++j)
       if (j < halo) {
         float v[V];
-        conv_input<T, V>(a, p.r, state, p.t0 - halo + j, c, v);
+        conv_input<T, V, ANY>(a, p.r, state, p.t0 - halo + j, c, v);
         shift_in<V, W>(win, v);
       }
     // g[t] of the segment's events and of the `halo` behind them completes dx[t - halo].  Behind the sequence's end g is zero.
@@ -245,8 +239,8 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
       if (p.t0 + u < t_end) {
-        nx[u] = *reinterpret_cast<const Pack<T, V>*>(x + u * step * a.ld_x);
-        ndy[u] = *reinterpret_cast<const Pack<T, V>*>(dy + u * step * a.ld_dy);
+        nx[u] = take<T, V, ANY>(x + u * step * a.ld_x, a.d - c);
+        ndy[u] = take<T, V, ANY>(dy + u * step * a.ld_dy, a.d - c);
       }
     // one event; INSIDE: it is the segment's own, and dx[t - halo] as well
     auto event = [&](auto inside, int t, int u) {
@@ -287,13 +281,13 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
             if (W != CONV_ANY || (j >= W - a.width && k == 2 * W - 1 - a.width - j))
 #pragma unroll
               for (int i = 0; i < V; ++i) o[i] = fmaf(w[k][i], gw[j][i], o[i]);
-        store_pack<T, V>(dx + (u - halo) * step * a.ld_y, o);
+        put<T, V, ANY>(dx + (u - halo) * step * a.ld_y, o, a.d - c);
       }
     };
     auto ask = [&](int t4, int u) {
       const int ahead = min(u + AHEAD, t_end - 1 - t4);   // (past the end: a row that is there)
-      nx[u] = *reinterpret_cast<const Pack<T, V>*>(x + ahead * step * a.ld_x);
-      ndy[u] = *reinterpret_cast<const Pack<T, V>*>(dy + ahead * step * a.ld_dy);
+      nx[u] = take<T, V, ANY>(x + ahead * step * a.ld_x, a.d - c);
+      ndy[u] = take<T, V, ANY>(dy + ahead * step * a.ld_dy, a.d - c);
     };
     auto on_to = [&]() {
       x += AHEAD * step * a.ld_x;
@@ -322,7 +316,7 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
     while (t4 < p.t1 + halo) border();
     if (p.last) {
       float zero[V] = {};
-      for (int t = p.r.len; t < p.r.slot; ++t) store_pack<T, V>(static_cast<T*>(a.y) + (p.r.begin + t) * a.ld_y + c, zero);
+      for (int t = p.r.len; t < p.r.slot; ++t) put<T, V, ANY>(static_cast<T*>(a.y) + (p.r.begin + t) * a.ld_y + c, zero, a.d - c);
     }
   }
   if (a.part == nullptr) return;
@@ -338,6 +332,7 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
     if (ty == 0 && on)
 #pragma unroll
       for (int i = 0; i < V; ++i) {
+        if (ANY && c + i >= a.d) continue;
         float sum = 0.0f;
         for (int r = 0; r < per_y; ++r) sum += acc[(r * a.per_x + tx) * V + i];
         if (j < W) part[(int64_t)(c + i) * a.width + j - (W - a.width)] = sum;
@@ -346,43 +341,20 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
   }
 }
 
-// The pack width: 16 bytes, or as much of it as divides the columns and every row's address allows.
-static int conv_pack(int dtype, int d, int64_t rows, const void* const* p, const int64_t* ld, int n) {
-  const int size = type_size(dtype);
-  for (int v = 16 / size; v > 1; v /= 2) {
-    bool ok = d % v == 0;
-    for (int i = 0; i < n; ++i) ok = ok && aligned_to(p[i], v * size) && (rows <= 1 || ld[i] % v == 0);
-    if (ok) return v;
-  }
-  return 1;
-}
-
-// f(T(), V, W) for a pack of V values
-template <class F> static void conv_shape(int dtype, int pack, int width, F f) {
+// f(T(), V, W, ANY): packs of 16 bytes, or of four values (FOUR: with eight the backward pass has two wavefronts to a vector
+// unit instead of three)
+template <bool FOUR, class F> static void conv_shape(int dtype, int width, int d, int64_t rows, const void* const* p, const int64_t* ld, int n, F f) {
   with_type(dtype, [&](auto t) {
-    auto by_width = [&](auto v) {
-      if (width == 2) f(t, v, std::integral_constant<int, 2>());
-      else if (width == 3) f(t, v, std::integral_constant<int, 3>());
-      else if (width == 4) f(t, v, std::integral_constant<int, 4>());
-      else f(t, v, std::integral_constant<int, CONV_ANY>());
+    constexpr int V = FOUR ? 4 : 16 / sizeof(t);
+    const std::integral_constant<int, V> v;
+    auto by_width = [&](auto any) {
+      if (width == 2) f(t, v, std::integral_constant<int, 2>(), any);
+      else if (width == 3) f(t, v, std::integral_constant<int, 3>(), any);
+      else if (width == 4) f(t, v, std::integral_constant<int, 4>(), any);
+      else f(t, v, std::integral_constant<int, CONV_ANY>(), any);
     };
-    if constexpr (sizeof(t) == 2)
-      if (pack == 8) return by_width(std::integral_constant<int, 8>());
-    if (pack >= 4) by_width(std::integral_constant<int, 4>());
-    else by_width(std::integral_constant<int, 1>());
-  });
-}
-// The same without packs of eight values, with which the backward pass has two wavefronts to a vector unit instead of three
-template <class F> static void conv_shape4(int dtype, int pack, int width, F f) {
-  with_type(dtype, [&](auto t) {
-    auto by_width = [&](auto v) {
-      if (width == 2) f(t, v, std::integral_constant<int, 2>());
-      else if (width == 3) f(t, v, std::integral_constant<int, 3>());
-      else if (width == 4) f(t, v, std::integral_constant<int, 4>());
-      else f(t, v, std::integral_constant<int, CONV_ANY>());
-    };
-    if (pack >= 4) by_width(std::integral_constant<int, 4>());
-    else by_width(std::integral_constant<int, 1>());
+    if (packs_fit(dtype, V, d, rows, p, ld, n)) by_width(std::false_type());
+    else by_width(std::true_type());
   });
 }
 
@@ -465,11 +437,11 @@ extern "C" int32_t tgnn_causal_conv_fwd(const tgnn_seqs* seqs, int32_t dtype, in
   a.ld_x = ld_x; a.ld_y = ld_y; a.d = d; a.width = width; a.n_states = n_states; a.silu = silu != 0;
   const void* p[] = {x, y, a.state_in, a.state_out};
   const int64_t ld[] = {ld_x, ld_y, d, d};
-  const int pack = conv_pack(dtype, d, seqs->n_rows, p, ld, 4);
   int rc = TGNN_OK;
-  conv_shape(dtype, pack, width, [&](auto t, auto v, auto wd) {
+  conv_shape<false>(dtype, width, d, seqs->n_rows, p, ld, 4, [&](auto t, auto v, auto wd, auto any) {
     using T = decltype(t);
     constexpr int V = decltype(v)::value, W = decltype(wd)::value;
+    constexpr bool ANY = decltype(any)::value;
     a.bits = conv_bits(*seqs, d, V, 4096);
     a.items = seg_total(*seqs, a.bits);
     a.per_x = conv_columns(d, V);
@@ -477,8 +449,8 @@ extern "C" int32_t tgnn_causal_conv_fwd(const tgnn_seqs* seqs, int32_t dtype, in
     unsigned grid;
     rc = conv_grid((a.items + per_y - 1) / per_y, tiles, &grid);
     if (rc != TGNN_OK) return;
-    if (a.per_x >= 64) hipLaunchKernelGGL((conv_fwd_kernel<T, V, W, true>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
-    else hipLaunchKernelGGL((conv_fwd_kernel<T, V, W, false>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    if (a.per_x >= 64) hipLaunchKernelGGL((conv_fwd_kernel<T, V, W, true, ANY>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    else hipLaunchKernelGGL((conv_fwd_kernel<T, V, W, false, ANY>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
   });
   if (rc != TGNN_OK) return rc;
   TGNN_LAUNCH_CHECK();
@@ -507,14 +479,13 @@ extern "C" int32_t tgnn_causal_conv_step(int32_t dtype, int64_t n_rows, int32_t 
   a.d = d; a.width = width; a.n_states = n_states; a.silu = silu != 0;
   const void* p[] = {x, y, a.state_in, a.state_out};
   const int64_t ld[] = {ld_x, ld_y, d, d};
-  const int pack = conv_pack(dtype, d, n_rows, p, ld, 4);
   int rc = TGNN_OK;
-  conv_shape(dtype, pack, width, [&](auto t, auto v, auto wd) {
+  conv_shape<false>(dtype, width, d, n_rows, p, ld, 4, [&](auto t, auto v, auto wd, auto any) {
     using T = decltype(t);
     constexpr int V = decltype(v)::value, W = decltype(wd)::value;
     unsigned grid;
-    rc = conv_grid((n_rows * (d / V) + 255) / 256, 1, &grid);
-    if (rc == TGNN_OK) hipLaunchKernelGGL((conv_step_kernel<T, V, W>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    rc = conv_grid((n_rows * ((d + V - 1) / V) + 255) / 256, 1, &grid);
+    if (rc == TGNN_OK) hipLaunchKernelGGL((conv_step_kernel<T, V, W, decltype(any)::value>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
   });
   if (rc != TGNN_OK) return rc;
   TGNN_LAUNCH_CHECK();
@@ -557,19 +528,19 @@ extern "C" int32_t tgnn_causal_conv_bwd(const tgnn_seqs* seqs, int32_t dtype, in
   a.d = d; a.width = width; a.n_states = n_states; a.silu = silu != 0;
   const void* p[] = {x, dy, dx, a.state_in};
   const int64_t ld[] = {ld_x, ld_dy, ld_dx, d};
-  const int pack = conv_pack(dtype, d, seqs->n_rows, p, ld, 4);
   int64_t workers = 0;
   if (seqs->n_seqs > 0) {
-    conv_shape4(dtype, pack, width, [&](auto t, auto v, auto wd) {
+    conv_shape<true>(dtype, width, d, seqs->n_rows, p, ld, 4, [&](auto t, auto v, auto wd, auto any) {
       using T = decltype(t);
       constexpr int V = decltype(v)::value, W = decltype(wd)::value;
+      constexpr bool ANY = decltype(any)::value;
       a.bits = conv_bits(*seqs, d, V, 3072);
       a.items = seg_total(*seqs, a.bits);
       a.per_x = conv_columns(d, V);
       const int per_y = 256 / a.per_x, tiles = (d + a.per_x * V - 1) / (a.per_x * V);
       workers = std::min<int64_t>((a.items + per_y - 1) / per_y, std::max(1, CONV_GRID / tiles));
-      if (a.per_x >= 64) hipLaunchKernelGGL((conv_bwd_kernel<T, V, W, true>), dim3((unsigned)(workers * tiles)), dim3(256), 0, s, a);
-      else hipLaunchKernelGGL((conv_bwd_kernel<T, V, W, false>), dim3((unsigned)(workers * tiles)), dim3(256), 0, s, a);
+      if (a.per_x >= 64) hipLaunchKernelGGL((conv_bwd_kernel<T, V, W, true, ANY>), dim3((unsigned)(workers * tiles)), dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((conv_bwd_kernel<T, V, W, false, ANY>), dim3((unsigned)(workers * tiles)), dim3(256), 0, s, a);
     });
     TGNN_LAUNCH_CHECK();
   }

@@ -6,7 +6,7 @@
 // Bound by memory: a row is read once (twice where it is wider than the registers of a workgroup hold) and written once.
 // G threads have a row between them, K packs of V values each, so that the second pass of the variance, and the second use of x
 // and dy in the backward pass, come from registers: 16 threads for up to 128 columns of float (a wavefront has four rows),
-// a wavefront up to 1,024, a workgroup beyond.  The backward pass walks over the rows with a fixed grid; a thread has the
+// a wavefront up to 1,024, a workgroup up to 8,192.  The backward pass walks over the rows with a fixed grid; a thread has the
 // same columns in every row and adds up its part of dw and db in registers, a workgroup adds up its threads' parts in LDS
 // and leaves one partial row.
 #include <math.h>
@@ -16,6 +16,8 @@
 #include "ops_device.h"
 
 namespace tgnn {
+
+constexpr int norm_threads(int g) { return g > 256 ? g : 256; }   // of a workgroup
 
 // sum over the G neighbouring threads that have a row
 template <int G> __device__ __forceinline__ float row_sum(float v, float* parts) {
@@ -43,31 +45,20 @@ struct NormArgs {
   float eps;
 };
 
-// V weights from column c on, or `other` ones
-template <int V> __device__ __forceinline__ void load_weights(const float* p, int c, float other, float (&w)[V]) {
-  if (p != nullptr) {
-    const FloatRun<V> r = *reinterpret_cast<const FloatRun<V>*>(p + c);
-#pragma unroll
-    for (int i = 0; i < V; ++i) w[i] = r.v[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i) w[i] = other;
-  }
-}
-
 // A group of threads walks over rows with the weights of its columns in registers and the next row on its way.
-template <class T, int V, int G, int K>
-__global__ __launch_bounds__(256) void norm_fwd_kernel(NormArgs a) {
-  __shared__ float parts[4];
-  constexpr int GROUPS = 256 / G;
+// ANY: rows at any address, of any number of columns.
+template <class T, int V, int G, int K, bool ANY>
+__global__ __launch_bounds__(norm_threads(G)) void norm_fwd_kernel(NormArgs a) {
+  __shared__ float parts[8];
+  constexpr int GROUPS = norm_threads(G) / G;
   const int c0 = (threadIdx.x % G) * V;
   const float inv = 1.0f / (float)a.cols;
   float w[K][V], b[K][V];
 #pragma unroll
   for (int k = 0; k < K; ++k)
     if (c0 + k * G * V < a.cols) {
-      load_weights<V>(a.weight, c0 + k * G * V, 1.0f, w[k]);
-      load_weights<V>(a.bias, c0 + k * G * V, 0.0f, b[k]);
+      take_floats<V>(a.weight ? a.weight + c0 + k * G * V : nullptr, a.cols - c0 - k * G * V, 1.0f, w[k]);
+      take_floats<V>(a.bias ? a.bias + c0 + k * G * V : nullptr, a.cols - c0 - k * G * V, 0.0f, b[k]);
     }
   const T* x = static_cast<const T*>(a.x) + c0;
   T* y = static_cast<T*>(a.y) + c0;
@@ -77,7 +68,7 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormArgs a) {
   auto ask = [&](int64_t r) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
-      if (c0 + k * G * V < a.cols) next[k] = *reinterpret_cast<const Pack<T, V>*>(x + r * a.ld_x + k * G * V);
+      if (c0 + k * G * V < a.cols) next[k] = take<T, V, ANY>(x + r * a.ld_x + k * G * V, a.cols - c0 - k * G * V);
   };
   if (row < a.rows) ask(row);
   for (; row < a.rows; row += step) {
@@ -96,7 +87,7 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormArgs a) {
     for (int k = 0; k < K; ++k)
       if (c0 + k * G * V < a.cols)
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum += (v[k][i] - mean) * (v[k][i] - mean);
+        for (int i = 0; i < V; ++i) sum += !ANY || c0 + k * G * V + i < a.cols ? (v[k][i] - mean) * (v[k][i] - mean) : 0.0f;
     const float rstd = 1.0f / sqrtf(row_sum<G>(sum, parts) * inv + a.eps);
     if (threadIdx.x % G == 0) {
       if (a.out_mean) a.out_mean[row] = mean;
@@ -108,7 +99,7 @@ __global__ __launch_bounds__(256) void norm_fwd_kernel(NormArgs a) {
       float o[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) o[i] = (v[k][i] - mean) * rstd * w[k][i] + b[k][i];
-      store_pack<T, V>(y + row * a.ld_y + k * G * V, o);
+      put<T, V, ANY>(y + row * a.ld_y + k * G * V, o, a.cols - c0 - k * G * V);
     }
   }
 }
@@ -134,10 +125,10 @@ __global__ __launch_bounds__(256) void norm_fwd_wide_kernel(NormArgs a) {
     y[c] = (T)(((float)x[c] - mean) * rstd * (a.weight ? a.weight[c] : 1.0f) + (a.bias ? a.bias[c] : 0.0f));
 }
 
-template <class T, int V, int G, int K>
-__global__ __launch_bounds__(256) void norm_bwd_kernel(NormArgs a) {
-  __shared__ float parts[4];
-  constexpr int GROUPS = 256 / G, W = G * K * V;   // row groups of a workgroup; columns its threads cover
+template <class T, int V, int G, int K, bool ANY>
+__global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(NormArgs a) {
+  __shared__ float parts[8];
+  constexpr int GROUPS = norm_threads(G) / G, W = G * K * V;   // row groups of a workgroup; columns its threads cover
   __shared__ float acc[GROUPS > 1 ? GROUPS : 1][GROUPS > 1 ? W : 1];
   const int c0 = (threadIdx.x % G) * V, group = threadIdx.x / G;
   float w[K][V], dw[K][V], db[K][V];
@@ -145,7 +136,7 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormArgs a) {
   for (int k = 0; k < K; ++k) {
 #pragma unroll
     for (int i = 0; i < V; ++i) w[k][i] = dw[k][i] = db[k][i] = 0.0f;   // (columns beyond the row weigh nothing)
-    if (c0 + k * G * V < a.cols) load_weights<V>(a.weight, c0 + k * G * V, 1.0f, w[k]);
+    if (c0 + k * G * V < a.cols) take_floats<V>(a.weight ? a.weight + c0 + k * G * V : nullptr, a.cols - c0 - k * G * V, 1.0f, w[k]);
   }
   const float inv = 1.0f / (float)a.cols;
   const T* x = static_cast<const T*>(a.x) + c0;
@@ -159,8 +150,8 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormArgs a) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
       if (c0 + k * G * V < a.cols) {
-        nx[k] = *reinterpret_cast<const Pack<T, V>*>(x + r * a.ld_x + k * G * V);
-        ndy[k] = *reinterpret_cast<const Pack<T, V>*>(dy + r * a.ld_dy + k * G * V);
+        nx[k] = take<T, V, ANY>(x + r * a.ld_x + k * G * V, a.cols - c0 - k * G * V);
+        ndy[k] = take<T, V, ANY>(dy + r * a.ld_dy + k * G * V, a.cols - c0 - k * G * V);
       }
     next_mean = a.mean[r];
     next_rstd = a.rstd[r];
@@ -177,9 +168,9 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormArgs a) {
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const bool in = c0 + k * G * V < a.cols;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
+        const bool in = c0 + k * G * V + (ANY ? i : 0) < a.cols;
         const float h = in ? (xh[k][i] - mean) * rstd : 0.0f, d = in ? g[k][i] : 0.0f;
         xh[k][i] = h;
         dw[k][i] += d * h;
@@ -197,7 +188,7 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormArgs a) {
       float o[V];
 #pragma unroll
       for (int i = 0; i < V; ++i) o[i] = rstd * (g[k][i] - s1 - xh[k][i] * s2);
-      store_pack<T, V>(dx + row * a.ld_y + k * G * V, o);
+      put<T, V, ANY>(dx + row * a.ld_y + k * G * V, o, a.cols - c0 - k * G * V);
     }
   }
   if (a.part == nullptr) return;
@@ -211,7 +202,7 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormArgs a) {
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[group][c0 + k * G * V + i] = q ? db[k][i] : dw[k][i];
       __syncthreads();
-      for (int c = threadIdx.x; c < a.cols; c += 256) {
+      for (int c = threadIdx.x; c < a.cols; c += norm_threads(G)) {
         float sum = 0.0f;
 #pragma unroll
         for (int r = 0; r < GROUPS; ++r) sum += acc[r][c];
@@ -222,7 +213,8 @@ __global__ __launch_bounds__(256) void norm_bwd_kernel(NormArgs a) {
       for (int k = 0; k < K; ++k)
         if (c0 + k * G * V < a.cols)
 #pragma unroll
-          for (int i = 0; i < V; ++i) part[q * a.cols + c0 + k * G * V + i] = q ? db[k][i] : dw[k][i];
+          for (int i = 0; i < V; ++i)
+            if (!ANY || c0 + k * G * V + i < a.cols) part[q * a.cols + c0 + k * G * V + i] = q ? db[k][i] : dw[k][i];
     }
   }
 }
@@ -265,24 +257,14 @@ __global__ __launch_bounds__(256) void norm_bwd_wide_weights_kernel(NormArgs a) 
   part[a.cols + c] = db;
 }
 
-// The pack width of a call: 16 bytes, or as much of it as divides the columns and every row's address allows.
-static int norm_pack(int dtype, int cols, int64_t rows, const void* const* p, const int64_t* ld, int n) {
-  const int size = type_size(dtype);
-  for (int v = 16 / size; v > 1; v /= 2) {
-    bool ok = cols % v == 0;
-    for (int i = 0; i < n; ++i) ok = ok && aligned_to(p[i], v * size) && (rows <= 1 || ld[i] % v == 0);
-    if (ok) return v;
-  }
-  return 1;
-}
-
 constexpr int NORM_FWD_GRID = 2048;   // workgroups of the forward pass: eight to a compute unit
 constexpr int NORM_GRID = 1024;       // workgroups of the backward pass (partial rows of dw and db), 768 where rows are
                                       // so wide that the partial rows' way counts and registers allow three to a compute unit
 constexpr int NORM_WIDE_PARTS = 64;   // the same where rows are wider than the registers
 
-// f(G, K) for the smallest group of threads that covers `packs` packs of a row; false: none does
-template <class F> static bool norm_shape(int64_t packs, F f) {
+// f(G, K) for the smallest group of threads that covers `packs` packs of V values of a row; false: none does.  (Four packs of eight
+// values and their sums are more than a thread's registers.)
+template <int V, class F> static bool norm_shape(int64_t packs, F f) {
   using std::integral_constant;
 #define TGNN_NORM_SHAPE(G, K) \
   if (packs <= (G) * (K)) { f(integral_constant<int, G>(), integral_constant<int, K>()); return true; }
@@ -292,17 +274,13 @@ template <class F> static bool norm_shape(int64_t packs, F f) {
   TGNN_NORM_SHAPE(64, 2)
   TGNN_NORM_SHAPE(64, 4)
   TGNN_NORM_SHAPE(256, 2)
-  TGNN_NORM_SHAPE(256, 4)
+  TGNN_NORM_SHAPE(512, 2)
+  if constexpr (V == 4) {
+    TGNN_NORM_SHAPE(512, 4)
+  }
 #undef TGNN_NORM_SHAPE
   return false;
 }
-template <class T, class F> static void norm_width(int pack, F f) {   // f(V)
-  constexpr int FULL = 16 / sizeof(T);
-  if (pack == FULL) f(std::integral_constant<int, FULL>());
-  else if (FULL == 8 && pack == 4) f(std::integral_constant<int, 4>());
-  else f(std::integral_constant<int, 1>());
-}
-
 static int64_t norm_grid(int64_t rows, int cols) {
   const int64_t most = cols > 1024 ? 768 : NORM_GRID;
   return rows < most ? (rows > 0 ? rows : 1) : most;
@@ -350,19 +328,18 @@ extern "C" int32_t tgnn_layer_norm_fwd(int32_t dtype, int64_t n_rows, int32_t n_
   a.rows = n_rows; a.ld_x = ld_x; a.ld_y = ld_y; a.cols = n_cols; a.eps = eps;
   const void* p[] = {x, y};
   const int64_t ld[] = {ld_x, ld_y};
-  const int pack = norm_pack(dtype, n_cols, n_rows, p, ld, 2);
+  const bool fit = packs_fit(dtype, 16 / type_size(dtype), n_cols, n_rows, p, ld, 2);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    norm_width<T>(pack, [&](auto v) {
-      constexpr int V = decltype(v)::value;
-      const bool fits = norm_shape((n_cols + V - 1) / V, [&](auto g, auto k) {
-        constexpr int G = decltype(g)::value, K = decltype(k)::value, PER = 256 / G;
-        const int64_t blocks = std::min<int64_t>((n_rows + PER - 1) / PER, NORM_FWD_GRID);
-        hipLaunchKernelGGL((norm_fwd_kernel<T, V, G, K>), dim3((unsigned)blocks), dim3(256), 0, s, a);
-      });
-      if (!fits) hipLaunchKernelGGL((norm_fwd_wide_kernel<T>), dim3((unsigned)n_rows), dim3(256), 0, s, a);
+    constexpr int V = 16 / sizeof(T);
+    const bool fits = norm_shape<V>((n_cols + V - 1) / V, [&](auto g, auto k) {
+      constexpr int G = decltype(g)::value, K = decltype(k)::value, THREADS = norm_threads(G), PER = THREADS / G;
+      const dim3 grid((unsigned)std::min<int64_t>((n_rows + PER - 1) / PER, NORM_FWD_GRID));
+      if (fit) hipLaunchKernelGGL((norm_fwd_kernel<T, V, G, K, false>), grid, dim3(THREADS), 0, s, a);
+      else hipLaunchKernelGGL((norm_fwd_kernel<T, V, G, K, true>), grid, dim3(THREADS), 0, s, a);
     });
+    if (!fits) hipLaunchKernelGGL((norm_fwd_wide_kernel<T>), dim3((unsigned)n_rows), dim3(256), 0, s, a);
   });
   TGNN_LAUNCH_CHECK();
   return TGNN_OK;
@@ -404,26 +381,25 @@ extern "C" int32_t tgnn_layer_norm_bwd(int32_t dtype, int64_t n_rows, int32_t n_
   a.rows = n_rows; a.ld_x = ld_x; a.ld_dy = ld_dy; a.ld_y = ld_dx; a.cols = n_cols;
   const void* p[] = {x, dy, dx};
   const int64_t ld[] = {ld_x, ld_dy, ld_dx};
-  const int pack = norm_pack(dtype, n_cols, n_rows, p, ld, 3);
+  const bool fit = packs_fit(dtype, 16 / type_size(dtype), n_cols, n_rows, p, ld, 3);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   int n_part = 0;
   if (n_rows > 0) {
     with_type(dtype, [&](auto t) {
       using T = decltype(t);
-      norm_width<T>(pack, [&](auto v) {
-        constexpr int V = decltype(v)::value;
-        const bool fits = norm_shape((n_cols + V - 1) / V, [&](auto g, auto k) {
-          constexpr int G = decltype(g)::value, K = decltype(k)::value, PER = 256 / G;
-          n_part = (int)norm_grid((n_rows + PER - 1) / PER, n_cols);
-          hipLaunchKernelGGL((norm_bwd_kernel<T, V, G, K>), dim3(n_part), dim3(256), 0, s, a);
-        });
-        if (fits) return;
-        if (weights) {   // (first: dx may be written over dy)
-          n_part = (int)(n_rows < NORM_WIDE_PARTS ? n_rows : NORM_WIDE_PARTS);
-          hipLaunchKernelGGL((norm_bwd_wide_weights_kernel<T>), dim3((n_cols + 255) / 256, n_part), dim3(256), 0, s, a);
-        }
-        hipLaunchKernelGGL((norm_bwd_wide_kernel<T>), dim3((unsigned)n_rows), dim3(256), 0, s, a);
+      constexpr int V = 16 / sizeof(T);
+      const bool fits = norm_shape<V>((n_cols + V - 1) / V, [&](auto g, auto k) {
+        constexpr int G = decltype(g)::value, K = decltype(k)::value, THREADS = norm_threads(G), PER = THREADS / G;
+        n_part = (int)norm_grid((n_rows + PER - 1) / PER, n_cols);
+        if (fit) hipLaunchKernelGGL((norm_bwd_kernel<T, V, G, K, false>), dim3(n_part), dim3(THREADS), 0, s, a);
+        else hipLaunchKernelGGL((norm_bwd_kernel<T, V, G, K, true>), dim3(n_part), dim3(THREADS), 0, s, a);
       });
+      if (fits) return;
+      if (weights) {   // (first: dx may be written over dy)
+        n_part = (int)(n_rows < NORM_WIDE_PARTS ? n_rows : NORM_WIDE_PARTS);
+        hipLaunchKernelGGL((norm_bwd_wide_weights_kernel<T>), dim3((n_cols + 255) / 256, n_part), dim3(256), 0, s, a);
+      }
+      hipLaunchKernelGGL((norm_bwd_wide_kernel<T>), dim3((unsigned)n_rows), dim3(256), 0, s, a);
     });
     TGNN_LAUNCH_CHECK();
   }

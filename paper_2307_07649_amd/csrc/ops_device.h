@@ -38,10 +38,63 @@ template <class T, int V> __device__ __forceinline__ void store_pack(T* p, const
 template <class T, int N> struct __attribute__((packed, aligned(sizeof(T)))) Run { T v[N]; };
 template <int N> using FloatRun = Run<float, N>;
 
+// V values of a row from p on, of which `left` are the row's own (the others: zeros, not written).  ANY: the row's values may begin
+// at any address of one and their number be no multiple of V; a pack that is all there is one access all the same, which the
+// hardware takes at any address.
+template <class T, int V, bool ANY> __device__ __forceinline__ Pack<T, V> take(const T* p, int left) {
+  Pack<T, V> q;
+  if constexpr (!ANY) {
+    q = *reinterpret_cast<const Pack<T, V>*>(p);
+  } else if (left >= V) {
+    const Run<T, V> r = *reinterpret_cast<const Run<T, V>*>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) q.v[i] = r.v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) q.v[i] = i < left ? p[i] : (T)0.0f;
+  }
+  return q;
+}
+template <class T, int V> __device__ __forceinline__ void unpack(const Pack<T, V>& q, float (&x)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) x[i] = (float)q.v[i];
+}
+template <class T, int V, bool ANY> __device__ __forceinline__ void put(T* p, const float (&x)[V], int left) {
+  if constexpr (!ANY) {
+    store_pack<T, V>(p, x);
+  } else if (left >= V) {
+    Run<T, V> r;
+#pragma unroll
+    for (int i = 0; i < V; ++i) r.v[i] = (T)x[i];
+    *reinterpret_cast<Run<T, V>*>(p) = r;
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < left) p[i] = (T)x[i];
+  }
+}
+// the same of floats, with `other` beyond the row or without a row
+template <int V> __device__ __forceinline__ void take_floats(const float* p, int left, float other, float (&w)[V]) {
+  if (p != nullptr && left >= V) {
+    const FloatRun<V> r = *reinterpret_cast<const FloatRun<V>*>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = r.v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = p != nullptr && i < left ? p[i] : other;
+  }
+}
+
 inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 inline bool spans_overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return a != nullptr && b != nullptr && na > 0 && nb > 0 && x < y + nb && y < x + na;
+}
+// whether packs of `pack` values fit all rows of n arrays: the columns and, from row to row, the addresses
+inline bool packs_fit(int dtype, int pack, int cols, int64_t rows, const void* const* p, const int64_t* ld, int n) {
+  bool ok = cols % pack == 0;
+  for (int i = 0; i < n; ++i) ok = ok && aligned_to(p[i], (size_t)pack * type_size(dtype)) && (rows <= 1 || ld[i] % pack == 0);
+  return ok;
 }
 // from the first value of a row array to behind its last one, in bytes
 inline size_t rows_span(int64_t rows, int64_t cols, int64_t ld, int size) {
