@@ -302,6 +302,15 @@ int32_t tgnn_eval_step_edge_class(tgnn_ctx* ctx, const tgnn_graph* g, tgnn_state
  * synchronises the device. */
 int32_t tgnn_set_optimizer(tgnn_ctx* ctx, int32_t kind, tgnn_params* m, tgnn_params* v, float beta1, float beta2, float eps);
 
+/* Gradient clipping of the in-step update (tgnn_train_step and its variants with lr != 0; SGD and Adam): from the next step on the
+ * update takes g * max_norm / norm in place of g wherever norm > max_norm, norm = sqrt(sum of the squares) over all gradients of
+ * the tensors that are updated (all but time_w, time_b; tgnn_clip_grads for gradients that are updated elsewhere).  The gradient
+ * tensors themselves keep the step's gradients.  max_norm = 0: no clipping (the default).  out_norm: device scalar that
+ * every step writes its norm to, or NULL.  A norm that is infinite or not a number scales nothing.  The rows of a
+ * co-trained static memory are not clipped.  The update leaves in two launches of its own behind the step's
+ * others (it rides in the last of them otherwise).  Synchronises the device. */
+int32_t tgnn_set_grad_clip(tgnn_ctx* ctx, float max_norm, float* out_norm);
+
 /* Co-trained static node memory (Sec. 3.1: the static memory as a learnable embedding table trained with the model
  * instead of a frozen pre-trained one).  From the next step on, every training step also back-propagates into the
  * static rows {static_w} of the nodes it touches (roots and supporting nodes):

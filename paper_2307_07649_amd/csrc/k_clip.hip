@@ -11,11 +11,12 @@
 #include <new>
 
 #include "ops_device.h"
+#include "writeback_device.h"
 
 namespace tgnn {
 
 constexpr int CLIP_TENSORS = 128;          // per launch: the table of a launch is part of its arguments (4 KB)
-constexpr int CLIP_BLOCKS = 1024;          // partial sums per launch: four workgroups for every compute unit
+constexpr int CLIP_BLOCKS = CLIP_PARTS;    // partial sums per launch: four workgroups for every compute unit
 constexpr int CLIP_CHUNK = 4096;           // elements a workgroup takes at a time
 
 struct ClipArgs {
@@ -118,16 +119,28 @@ template <class T> __device__ __forceinline__ void chunk_scale(const T* p, T* o,
 }
 
 // A norm that is no finite number scales nothing: the gradients stay (or are copied) as they are, and the norm says so.
+__device__ __forceinline__ float clip_scale(double norm, float max_norm) {
+  return norm > (double)max_norm && norm < HUGE_VAL ? (float)((double)max_norm / norm) : 1.0f;
+}
+
 __global__ __launch_bounds__(256) void clip_scale_kernel(ClipArgs a) {
   const double norm = norm_of_parts(a.part, a.n_part);
   if (a.write_norm && blockIdx.x == 0 && threadIdx.x == 0) *a.out_norm = (float)norm;
-  const float scale = norm > (double)a.max_norm && norm < HUGE_VAL ? (float)((double)a.max_norm / norm) : 1.0f;
+  const float scale = clip_scale(norm, a.max_norm);
   clip_chunks(a, [&](int t, int type, int64_t at, int n) {
     if (scale == 1.0f && a.dst[t] == a.src[t]) return;
     if (type == TGNN_F32) chunk_scale(static_cast<const float*>(a.src[t]) + at, static_cast<float*>(a.dst[t]) + at, n, scale);
     else if (type == TGNN_BF16) chunk_scale(static_cast<const bf16*>(a.src[t]) + at, static_cast<bf16*>(a.dst[t]) + at, n, scale);
     else chunk_scale(static_cast<const f16*>(a.src[t]) + at, static_cast<f16*>(a.dst[t]) + at, n, scale);
   });
+}
+
+// The update of a training step with clipped gradients: as in the scaled copy, every workgroup adds up the partial sums.
+__global__ __launch_bounds__(256) void clipped_update_kernel(const SgdSet* set, const AdamSet* adam, const double* part, int n_part,
+                                                             float max_norm, float lr, float* out_norm) {
+  const double norm = norm_of_parts(part, n_part);
+  if (out_norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *out_norm = (float)norm;
+  param_update_block(*set, adam, blockIdx.x >> 6, blockIdx.x & 63, lr, clip_scale(norm, max_norm));
 }
 
 static int check_tensors(int32_t n, const void* const* g, const int64_t* numel, const int32_t* dtype) {
@@ -207,6 +220,22 @@ static int norm_launches(int32_t n, const void* const* g, const int64_t* numel, 
   });
   if (rc == TGNN_OK && !fits) return set_error(TGNN_E_WORKSPACE, "the workspace is too small for the list's partial sums");
   return rc;
+}
+
+int clipped_update(const SgdSet& host, const SgdSet* set, const AdamSet* adam, double* part, float max_norm, float lr, float* out_norm,
+                   hipStream_t s) {
+  static_assert(sizeof(SgdSet::p) / sizeof(float*) <= CLIP_TENSORS, "one launch has all tensors of a training step");
+  int64_t numel[CLIP_TENSORS];
+  int32_t dtype[CLIP_TENSORS];
+  for (int i = 0; i < host.cnt; ++i) { numel[i] = host.n[i]; dtype[i] = TGNN_F32; }
+  ClipArgs a = {};
+  int n_part = 0;
+  if (int rc = norm_launches(host.cnt, reinterpret_cast<const void* const*>(host.g), numel, dtype, a, part,
+                             CLIP_PARTS * (int64_t)sizeof(double), s, n_part))
+    return rc;
+  hipLaunchKernelGGL(clipped_update_kernel, dim3(64 * host.cnt), dim3(256), 0, s, set, adam, part, n_part, max_norm, lr, out_norm);
+  TGNN_LAUNCH_CHECK();
+  return TGNN_OK;
 }
 
 }  // namespace tgnn

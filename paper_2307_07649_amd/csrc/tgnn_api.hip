@@ -104,7 +104,7 @@ static void layout(const Dims& d, Ws& w, Bump& b) {
   w.sorted_row = b.take<int32_t>(S); w.sort_total = b.take<int32_t>(1);
   w.ds_row = b.take<float>(S * d.ldh);
   w.dstat = d.ds > 0 ? b.take<float>(S * d.ldst) : nullptr;
-  w.adam_dev = b.take<AdamSet>(1); w.adam_t = b.take<int32_t>(1);
+  w.adam_dev = b.take<AdamSet>(1); w.adam_t = b.take<int32_t>(1); w.clip_part = b.take<double>(CLIP_PARTS);
   w.bs_dev = b.take<BatchSet>(1);
   w.sgd_dev = b.take<SgdSet>(1);
   w.q_part = b.take<float>((size_t)QPHI_BLOCKS * d.dO);
@@ -1260,9 +1260,10 @@ static int enqueue_step(tgnn_ctx* ctx, const tgnn_graph* g, tgnn_state* st, cons
     tg.delta = w.delta; tg.w = p->time_w; tg.b = p->time_b; tg.g_w = grads->time_w; tg.g_b = grads->time_b;
     const NtProblem pr = nt_rows(nt_live(nt_problem(w.dgi, d.ld3, w.WihT_phi, d.ld3, nullptr, nullptr, d.ldt, U, d.dt, d.ld3, d.ldt,
                                                     false, w.ucount, RowAdd(), tg), 3 * d.dm), U_est);
+    const bool rides = lr != 0.0f && ctx->clip_norm == 0.0f;   // (a clipped update needs the norm of all gradients first)
     WbArgs wb = writeback_args(d, w.bs_dev, bs.total, st, w.winkey, w.epoch, w.Xrow, d.ldxr, w.tau, w.slot_row, nullptr,
-                               nullptr, nullptr, nullptr, out_winner, lr != 0.0f ? w.sgd_dev : nullptr, sgd_set.cnt, lr);
-    if (ctx->adam && lr != 0.0f) wb.adam = w.adam_dev;
+                               nullptr, nullptr, nullptr, out_winner, rides ? w.sgd_dev : nullptr, sgd_set.cnt, lr);
+    if (ctx->adam && rides) wb.adam = w.adam_dev;
     if (ctx->train_static && d.ds > 0) {
       StatUpd& u = wb.stat;
       u.drow = w.dstat; u.ld = d.ldst; u.ds = d.ds; u.N = d.N; u.ulist = w.ulist; u.ucount = w.ucount;
@@ -1271,6 +1272,9 @@ static int enqueue_step(tgnn_ctx* ctx, const tgnn_graph* g, tgnn_state* st, cons
     }
     gemm_nt_group(&pr, 1, s, &wb);
   }
+  if (lr != 0.0f && ctx->clip_norm != 0.0f)
+    if (int rc = clipped_update(sgd_set, w.sgd_dev, ctx->adam ? w.adam_dev : nullptr, w.clip_part, ctx->clip_norm, lr, ctx->clip_out, s))
+      return rc;
   tm.end(17);
   if (out_logits)
     TGNN_HIP_CHECK(hipMemcpyAsync(out_logits, w.logits, sizeof(float) * n_logits, hipMemcpyDeviceToDevice, s));
@@ -1307,6 +1311,17 @@ int32_t tgnn_set_optimizer(tgnn_ctx* ctx, int32_t kind, tgnn_params* m, tgnn_par
   TGNN_HIP_CHECK(hipMemcpy(ctx->w.adam_dev, &a, sizeof(a), hipMemcpyHostToDevice));
   TGNN_HIP_CHECK(hipMemset(ctx->w.adam_t, 0, sizeof(int32_t)));
   ctx->adam = true;
+  return TGNN_OK;
+}
+
+int32_t tgnn_set_grad_clip(tgnn_ctx* ctx, float max_norm, float* out_norm) {
+  if (ctx == nullptr) return set_error(TGNN_E_NULL_PTR, "ctx is NULL");
+  if (!(max_norm >= 0.0f)) return set_error(TGNN_E_INVALID_ARG, "max_norm = %g: a positive number, or 0 for no clipping", (double)max_norm);
+  if ((reinterpret_cast<uintptr_t>(out_norm) & 3u) != 0) return set_error(TGNN_E_MISALIGNED, "out_norm is not aligned to its type");
+  TGNN_HIP_CHECK(hipDeviceSynchronize());
+  drop_graphs(ctx);
+  ctx->clip_norm = max_norm;
+  ctx->clip_out = max_norm != 0.0f ? out_norm : nullptr;
   return TGNN_OK;
 }
 

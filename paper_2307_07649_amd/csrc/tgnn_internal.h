@@ -88,6 +88,7 @@ struct Ws {
   float* dstat;                                // [maxS, ldst] gradient reaching the static columns per row (co-training)
   struct AdamSet* adam_dev;                    // device copy of the Adam moment pointers and constants
   int32_t* adam_t;                             // [1] Adam steps so far
+  double* clip_part;                           // [CLIP_PARTS] partial sums of the gradients' squares
   BatchSet* bs_dev;                            // device copy of the step's batch descriptors
   struct SgdSet* sgd_dev;                      // device copy of the parameter/gradient pointer table
   float* q_part;                               // [QPHI_BLOCKS, d_o] column sums of dq per block of roots
@@ -192,6 +193,8 @@ struct tgnn_ctx {
   bool train_static = false;       // tgnn_train_static
   float* grad_static = nullptr;
   float lr_static = 0.f;
+  float clip_norm = 0.f;           // tgnn_set_grad_clip: largest gradient norm of the in-step update, 0: any
+  float* clip_out = nullptr;       // ... where the norm goes
 };
 
 namespace tgnn {
@@ -212,6 +215,12 @@ struct SgdSet {
   int n[20];
   int cnt;
 };
+
+// The in-step update with the gradients scaled to a norm of at most max_norm (k_clip.hip): host table of the tensors, the
+// same table and Adam's on the device, CLIP_PARTS partial sums.
+constexpr int CLIP_PARTS = 1024;
+int clipped_update(const SgdSet& host, const SgdSet* set, const struct AdamSet* adam, double* part, float max_norm, float lr,
+                   float* out_norm, hipStream_t s);
 
 // Adam's moment tensors and constants (tgnn_set_optimizer), in the order of the SGD pointer table.
 struct AdamSet {

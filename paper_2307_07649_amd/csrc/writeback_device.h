@@ -85,6 +85,31 @@ __device__ __forceinline__ void rank_sum_block(const RankSum& a, int block) {
   if (threadIdx.x == 0) atomicAdd(a.rr_sum, sum[0] + sum[1] + sum[2] + sum[3]);
 }
 
+// The optimiser's update: 64 blocks per tensor, block x of tensor t.  `scale`: of the gradients (1 unless they are clipped).
+__device__ __forceinline__ void param_update_block(const SgdSet& set, const AdamSet* adam, int t, int x, float lr, float scale) {
+  float* p = set.p[t];
+  const float* g = set.g[t];
+  const int n = set.n[t];
+  if (adam != nullptr) {   // Adam with bias correction; the step count and the corrections in double
+    const AdamSet& ad = *adam;
+    float* m = ad.m[t];
+    float* v = ad.v[t];
+    const double steps = (double)*ad.t;
+    const float c1 = (float)(1.0 / (1.0 - pow((double)ad.beta1, steps)));
+    const float c2 = (float)(1.0 / (1.0 - pow((double)ad.beta2, steps)));
+    for (int i = x * 256 + threadIdx.x; i < n; i += 64 * 256) {
+      const float gi = g[i] * scale;
+      const float mi = ad.beta1 * m[i] + (1.0f - ad.beta1) * gi;
+      const float vi = ad.beta2 * v[i] + (1.0f - ad.beta2) * gi * gi;
+      m[i] = mi;
+      v[i] = vi;
+      p[i] -= lr * (mi * c1) / (sqrtf(vi * c2) + ad.eps);
+    }
+    return;
+  }
+  for (int i = x * 256 + threadIdx.x; i < n; i += 64 * 256) p[i] -= lr * (g[i] * scale);
+}
+
 // block: 0 .. wb_total_blocks(a) - 1
 __device__ __forceinline__ void wb_sgd_block(const WbArgs& a, int block) {
   if (block >= a.wb_blocks) {
@@ -95,28 +120,7 @@ __device__ __forceinline__ void wb_sgd_block(const WbArgs& a, int block) {
       else if (a.rr.rank != nullptr) rank_sum_block(a.rr, extra - n_sgd - a.stat.blocks);
       return;
     }
-    const int t = extra >> 6, x = extra & 63;
-    float* p = a.sgd->p[t];
-    const float* g = a.sgd->g[t];
-    const int n = a.sgd->n[t];
-    if (a.adam != nullptr) {   // Adam with bias correction; the step count and the corrections in double
-      const AdamSet& ad = *a.adam;
-      float* m = ad.m[t];
-      float* v = ad.v[t];
-      const double steps = (double)*ad.t;
-      const float c1 = (float)(1.0 / (1.0 - pow((double)ad.beta1, steps)));
-      const float c2 = (float)(1.0 / (1.0 - pow((double)ad.beta2, steps)));
-      for (int i = x * 256 + threadIdx.x; i < n; i += 64 * 256) {
-        const float gi = g[i];
-        const float mi = ad.beta1 * m[i] + (1.0f - ad.beta1) * gi;
-        const float vi = ad.beta2 * v[i] + (1.0f - ad.beta2) * gi * gi;
-        m[i] = mi;
-        v[i] = vi;
-        p[i] -= a.lr * (mi * c1) / (sqrtf(vi * c2) + ad.eps);
-      }
-      return;
-    }
-    for (int i = x * 256 + threadIdx.x; i < n; i += 64 * 256) p[i] -= a.lr * g[i];
+    param_update_block(*a.sgd, a.adam, extra >> 6, extra & 63, a.lr, 1.0f);
     return;
   }
   if (a.vec == 4) wb_scatter_block<4>(a, block);

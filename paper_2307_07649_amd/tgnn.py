@@ -102,6 +102,7 @@ _SIGS = {
     "tgnn_train_steps": (_I, [_P, C.POINTER(tgnn_graph), C.POINTER(tgnn_state), C.POINTER(tgnn_params),
                               C.POINTER(tgnn_params), _I, C.POINTER(tgnn_batch), _I, C.c_float, _P, _P]),
     "tgnn_set_optimizer": (_I, [_P, _I, C.POINTER(tgnn_params), C.POINTER(tgnn_params), C.c_float, C.c_float, C.c_float]),
+    "tgnn_set_grad_clip": (_I, [_P, C.c_float, _P]),
     "tgnn_train_static": (_I, [_P, _I, _P, C.c_float]),
     "tgnn_debug_read": (_I, [_P, _I, _P, C.c_int64, _P]),
     "tgnn_debug_copy": (_I, [_P, _P, C.c_int64, _P]),
@@ -701,6 +702,11 @@ class Context:
         self._opt = (m, v)      # keeps the moment tensors alive
         _check(_lib.tgnn_set_optimizer(self.h, kind, C.byref(m.c) if m else None, C.byref(v.c) if v else None, beta1, beta2,
                                        eps))
+
+    def tgnn_set_grad_clip(self, max_norm, out_norm=None):
+        """max_norm of the in-step update's gradients, 0: none; out_norm: float32 device tensor [1], every step's norm."""
+        self._clip_norm = out_norm      # keeps it alive
+        _check(_lib.tgnn_set_grad_clip(self.h, max_norm, _ptr(out_norm)))
 
     def tgnn_train_static(self, enable, grad_static=None, lr_static=0.0):
         self._gstat = grad_static
