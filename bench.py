@@ -12,6 +12,7 @@ The headline (`value`) is the largest single-GPU configuration, C4: 16,682 nodes
 from __future__ import annotations
 
 import argparse
+import gc
 import json
 import os
 import re
@@ -279,10 +280,15 @@ def run_config(tgnn, torch, P, args, detail):
         torch.cuda.synchronize()
         ctx.tgnn_profile_enable(roof_mask)    # drops the warm-up's records
         ctx.tgnn_profile_every(every)
+        # A full pass of Python's collector over everything that is loaded takes 40 ms, as long as 400 steps of the smallest
+        # workload; where it falls depends on how many objects the imports have made.  It has its pass here and none below.
+        gc.collect()
+        gc.disable()
         t0 = time.perf_counter()
         per_step = run_steps(args.warmup, args.warmup + args.steps)
         torch.cuda.synchronize()
         dt = time.perf_counter() - t0
+        gc.enable()
         assert len(per_step) == args.steps
         ev = sum(per_step)
         timed = per_step[::every] if roof_mask else []     # the library times every `every`-th step, from the first on
