@@ -534,7 +534,7 @@ extern "C" int32_t tgnn_causal_conv_bwd(const tgnn_seqs* seqs, int32_t dtype, in
       using T = decltype(t);
       constexpr int V = decltype(v)::value, W = decltype(wd)::value;
       constexpr bool ANY = decltype(any)::value;
-      a.bits = conv_bits(*seqs, d, V, 3072);
+      a.bits = conv_bits(*seqs, d, V, 3000);
       a.items = seg_total(*seqs, a.bits);
       a.per_x = conv_columns(d, V);
       const int per_y = 256 / a.per_x, tiles = (d + a.per_x * V - 1) / (a.per_x * V);
