@@ -48,12 +48,14 @@ struct ScanArgs {
   void *y, *dx, *ddt, *dz, *dB, *dC;
   float* saved;                         // [chunks, d, n] state before every chunk
   float *seg_state, *seg_delta;         // [segments, d, n], [segments, d]
-  float* part;                          // [workers, d n + 2 d] partial sums of dA, dD, dbias
+  float* part;                          // [workers, d n + 2 d] partial sums of dA, dD, dbias (of slices: dA alone)
+  float* part_y;                        // [3, slices, rows, d] the slices' parts of y0, s1, s2
   float* part_bc;                       // [column tiles of a group, rows, 2, groups n]; NULL: dB and dC are written directly
   int64_t ld_x, ld_dt, ld_b, ld_c, ld_z, ld_dy, ld_y, ld_dx, ld_ddt, ld_dz, ld_db, ld_dc, items;
   int d, n, groups, dg, n_states, softplus;
   int bits;                             // a segment has 2^bits events; WHOLE: sequences are not cut
   int tiles;                            // column tiles of a group
+  int slices;                           // of the states
 };
 
 // log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|); log1p(e) = 2 artanh(s), s = e / (2 + e) <= 1/3, by its series up to s^15
@@ -77,27 +79,33 @@ __device__ __forceinline__ int64_t state_of(const ScanArgs& a, int s) {
   return i >= 0 && i < a.n_states ? i : -1;
 }
 
-// N states of a column from and to memory
+// N states of a column from and to memory, four at a time at any address: a column's neighbours in the wavefront are n floats away, so
+// that every instruction touches 64 lines, and one float per instruction is four times as many of them (lists of one event,
+// 623 columns of 63 states: 253 us a forward call with saved states, and 618).
+typedef float Quad __attribute__((ext_vector_type(4), aligned(4)));
 template <int NP> __device__ __forceinline__ void load_states(const float* p, int n, float (&h)[NP]) {
-  if (n == NP && NP % 4 == 0 && (n & 3) == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+  static_assert(NP % 4 == 0, "in fours");
 #pragma unroll
-    for (int i = 0; i + 3 < NP; i += 4) {
-      const float4 v = *reinterpret_cast<const float4*>(p + i);
+  for (int i = 0; i < NP; i += 4) {
+    if (i + 4 <= n) {
+      const Quad v = *reinterpret_cast<const Quad*>(p + i);
       h[i] = v.x; h[i + 1] = v.y; h[i + 2] = v.z; h[i + 3] = v.w;
-    }
-  } else {
+    } else {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) h[i] = i < n ? p[i] : 0.0f;
+      for (int k = i; k < i + 4; ++k) h[k] = k < n ? p[k] : 0.0f;
+    }
   }
 }
 template <int NP> __device__ __forceinline__ void store_states(float* p, int n, const float (&h)[NP]) {
-  if (n == NP && NP % 4 == 0 && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
 #pragma unroll
-    for (int i = 0; i + 3 < NP; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(h[i], h[i + 1], h[i + 2], h[i + 3]);
-  } else {
+  for (int i = 0; i < NP; i += 4) {
+    if (i + 4 <= n) {
+      *reinterpret_cast<Quad*>(p + i) = Quad{h[i], h[i + 1], h[i + 2], h[i + 3]};
+    } else {
 #pragma unroll
-    for (int i = 0; i < NP; ++i)
-      if (i < n) p[i] = h[i];
+      for (int k = i; k < i + 4; ++k)
+        if (k < n) p[k] = h[k];
+    }
   }
 }
 
@@ -332,8 +340,9 @@ __device__ __forceinline__ float rows_sum(float u, float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// Wavefronts of a workgroup: as many as 48 KB of LDS hold the states of (three workgroups to a compute unit)
-constexpr int bwd_waves(int np) { return np <= 4 ? 4 : np == 8 ? 2 : 1; }
+constexpr int BWD_WAVES = 4, BWD_COLS = 16 * BWD_WAVES;   // wavefronts and columns of a workgroup
+constexpr int FINISH_BITS = 3;
+constexpr int SLICE = 16;                                 // states of a column that a workgroup has at most
 
 // v[e][i] of four events and NP states, summed over the wavefront's 16 columns: every lane gets the sums of its four states for
 // one event, event_of_sum(lane)
@@ -347,25 +356,29 @@ template <int NP> __device__ __forceinline__ void column_sums(const float (&v)[4
 }
 __device__ __forceinline__ int event_of_sum(int lane) { return 2 * (lane >> 5) + (lane >> 4 & 1); }
 
-// A workgroup: 16 columns per wavefront of one group, over the pieces worker, worker + workers, ...
-template <class T, int NP, bool USUAL>
-__global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_kernel(ScanArgs a) {
-  constexpr int WAVES = bwd_waves(NP), THREADS = 64 * WAVES, N4 = 4 * NP, STAGE = CHUNK * N4 / THREADS > 0 ? CHUNK * N4 / THREADS : 1;
-  constexpr bool AHEAD = STAGE <= 2;                 // the next chunk's B, C and states are asked for a chunk ahead
+// A workgroup: 16 columns per wavefront of one group, over the pieces worker, worker + workers, ...  With more than 16 states (SLICED)
+// it has 16 of them, n0 .. n0 + 15, and leaves its part of the sums over the states (y0, s1, s2) for scan_finish_kernel.  (With all 64
+// states of a column in four lanes, spilled, one wavefront to a vector unit, forward and backward over 10,000 events of 86 columns and 37
+// states took 419 us, now 235; 1,126 lists of one event, 623 columns, 63 states: 1,311 and 594.)
+template <class T, int NP, bool USUAL, bool SLICED>
+__global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_bwd_kernel(ScanArgs a) {
+  constexpr int WAVES = BWD_WAVES, THREADS = 64 * WAVES, N4 = 4 * NP, STAGE = CHUNK * N4 / THREADS > 0 ? CHUNK * N4 / THREADS : 1;
   __shared__ float bound[CHUNK / 4][THREADS * NP];   // a lane's states before every fourth event
   __shared__ float sB[CHUNK * N4], sC[CHUNK * N4];   // of the chunk's events
   __shared__ float red[WAVES][2][CHUNK * N4];        // dB, dC summed over a wavefront's columns
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane & 3;
-  const int all = a.groups * a.tiles, tile = blockIdx.x % all, worker = blockIdx.x / all, workers = gridDim.x / all;
-  const int grp = tile / a.tiles, sub = tile - grp * a.tiles;
-  const int col = sub * 16 * WAVES + wave * 16 + (lane >> 2);
+  const int per = a.groups * a.tiles, all = SLICED ? per * a.slices : per;
+  const int worker = blockIdx.x / all, workers = gridDim.x / all, at_all = blockIdx.x - worker * all, slice = SLICED ? at_all / per : 0;
+  const int tile = at_all - slice * per, grp = tile / a.tiles, sub = tile - grp * a.tiles;
+  const int n0 = slice * SLICE, n_here = SLICED ? min(a.n - n0, SLICE) : a.n;
+  const int col = sub * BWD_COLS + wave * 16 + (lane >> 2);
   const bool on = col < a.dg, full = __all(on), odd = (q & 1) != 0, high = (q & 2) != 0;
   const bool soft = USUAL || a.softplus, gated = USUAL || a.z != nullptr, newest = a.q.newest_first != 0;
   const unsigned c = grp * a.dg + (on ? col : a.dg - 1);
   float A[NP], dA[NP];
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
-    A[i] = q * NP + i < a.n ? a.A[(int64_t)c * a.n + q * NP + i] : 0.0f;
+    A[i] = q * NP + i < n_here ? a.A[(int64_t)c * a.n + n0 + q * NP + i] : 0.0f;
     dA[i] = 0.0f;
   }
   const float bias = a.bias ? a.bias[c] : 0.0f, D = a.D ? a.D[c] : 0.0f;
@@ -381,7 +394,7 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_
       p = piece_at(a.q, (int)item, a.bits);
       if (p.none) continue;
       if (p.last && p.r.slot > p.r.len) {
-        for (int t = p.r.len + q; on && t < p.r.slot; t += 4) {
+        for (int t = p.r.len + q; on && slice == 0 && t < p.r.slot; t += 4) {
           const int64_t row = p.r.begin + t;
           (static_cast<T*>(a.dx) + row * a.ld_dx)[c] = (T)0.0f;
           (static_cast<T*>(a.ddt) + row * a.ld_ddt)[c] = (T)0.0f;
@@ -389,10 +402,10 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_
         }
         if (sub == 0)
           for (int t = p.r.len + wave; t < p.r.slot; t += WAVES)
-            for (int n = lane; n < a.n; n += 64) {
+            for (int n = lane; n < n_here; n += 64) {
               const int64_t row = p.r.begin + t;
-              (static_cast<T*>(a.dB) + row * a.ld_db)[grp * a.n + n] = (T)0.0f;
-              (static_cast<T*>(a.dC) + row * a.ld_dc)[grp * a.n + n] = (T)0.0f;
+              (static_cast<T*>(a.dB) + row * a.ld_db)[grp * a.n + n0 + n] = (T)0.0f;
+              (static_cast<T*>(a.dC) + row * a.ld_dc)[grp * a.n + n0 + n] = (T)0.0f;
             }
       }
       if (p.t0 < p.t1) {
@@ -417,20 +430,20 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_
       for (int r = 0; r < STAGE; ++r) {
         const int i = tid + r * THREADS, e = i / N4, n = i % N4;
         rb[r] = rc[r] = (T)0.0f;
-        if (e < n_ev && n < a.n) {
+        if (e < n_ev && n < n_here) {
           const int64_t row = seq_row(a.q, p.r, tb + e);
-          rb[r] = (static_cast<const T*>(a.B) + row * a.ld_b)[grp * a.n + n];
-          rc[r] = (static_cast<const T*>(a.C) + row * a.ld_c)[grp * a.n + n];
+          rb[r] = (static_cast<const T*>(a.B) + row * a.ld_b)[grp * a.n + n0 + n];
+          rc[r] = (static_cast<const T*>(a.C) + row * a.ld_c)[grp * a.n + n0 + n];
         }
       }
-      const float* sv = a.saved + ((int64_t)(seg_base(a.q, p.s, CHUNK_BITS) + tb / CHUNK) * a.d + c) * a.n + q * NP;
+      const float* sv = a.saved + ((int64_t)(seg_base(a.q, p.s, CHUNK_BITS) + tb / CHUNK) * a.d + c) * a.n + n0 + q * NP;
 #pragma unroll
-      for (int i = 0; i < NP; ++i) hn[i] = on && q * NP + i < a.n ? sv[i] : 0.0f;
+      for (int i = 0; i < NP; ++i) hn[i] = on && q * NP + i < n_here ? sv[i] : 0.0f;
     };
     auto ask_back = [&](const Piece& p) {   // what reaches a piece from behind
 #pragma unroll
       for (int i = 0; i < NP; ++i)
-        g[i] = a.bits != WHOLE && on && q * NP + i < a.n ? a.seg_state[((int64_t)p.slot * a.d + c) * a.n + q * NP + i] : 0.0f;
+        g[i] = a.bits != WHOLE && on && q * NP + i < n_here ? a.seg_state[((int64_t)p.slot * a.d + c) * a.n + n0 + q * NP + i] : 0.0f;
     };
     struct Own { T x, dt, z, dy; };
     auto low_row = [&](const Piece& p, int t) { return p.r.begin + (newest ? p.r.len - 4 - t : t); };   // of the events t .. t + 3
@@ -449,13 +462,12 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_
 
     Own nx;
     if (more) {
-      if (AHEAD) ask_chunk(p, tb);
+      ask_chunk(p, tb);
       ask_back(p);
       ask(p, tb, p.t1 - tb <= 4, nx);
     }
     while (more) {
       const int n_ev = min(CHUNK, p.t1 - tb), n_sub = (n_ev + 3) / 4;
-      if (!AHEAD) ask_chunk(p, tb);
 #pragma unroll
       for (int r = 0; r < STAGE; ++r)
         if (CHUNK * N4 >= THREADS || tid < CHUNK * N4) {
@@ -490,7 +502,7 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_
         more = advance(np);
         next_tb = more ? np.t0 + (np.t1 - 1 - np.t0) / CHUNK * CHUNK : 0;
       }
-      if (AHEAD && more) ask_chunk(np, next_tb);
+      if (more) ask_chunk(np, next_tb);
       // and back, four events at a time
       for (int j = n_sub - 1; j >= 0; --j) {
         const Own v = nx;
@@ -548,6 +560,17 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_
 #pragma unroll
           for (int i = 0; i < NP; ++i) red[wave][0][at + i] = sum[i];
         const float t1 = quad_scatter_sum(s1, odd, high), t2 = quad_scatter_sum(s2, odd, high);
+        if constexpr (SLICED) {
+          const float y0 = quad_scatter_sum(y, odd, high);
+          if (there) {
+            float* o = a.part_y + ((int64_t)slice * a.q.n_rows + low_row(p, tb + 4 * j) + up) * a.d + c;
+            const int64_t all_rows = (int64_t)a.slices * a.q.n_rows * a.d;
+            o[0] = y0;
+            o[all_rows] = t1;
+            o[2 * all_rows] = t2;
+          }
+          continue;
+        }
         const float dd = fmaf(x, t1, t2), draw = soft ? dd * sigmoid(raw) : dd;
         float dz = 0.0f;
         if (gated) dz = dy * fmaf(D, x, quad_scatter_sum(y, odd, high)) * (sg * fmaf(z, 1.0f - sg, 1.0f));
@@ -564,12 +587,12 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_
       __syncthreads();
       for (int i = tid; i < n_ev * 2 * N4; i += THREADS) {
         const int kind = i >= n_ev * N4, at = kind ? i - n_ev * N4 : i, e = at / N4, n = at % N4;
-        if (n >= a.n) continue;
+        if (n >= n_here) continue;
         float sum = 0.0f;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) sum += red[w][kind][at];
         const int64_t row = seq_row(a.q, p.r, tb + e);
-        const int k = grp * a.n + n;
+        const int k = grp * a.n + n0 + n;
         if (a.part_bc != nullptr) a.part_bc[((sub * a.q.n_rows + row) * 2 + kind) * a.groups * a.n + k] = sum;
         else if (kind == 0) (static_cast<T*>(a.dB) + row * a.ld_db)[k] = (T)sum;
         else (static_cast<T*>(a.dC) + row * a.ld_dc)[k] = (T)sum;
@@ -579,7 +602,7 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_
     }
   }
   if (a.part == nullptr) return;
-  float* part = a.part + (int64_t)worker * ((int64_t)a.d * a.n + 2 * a.d);
+  float* part = a.part + (int64_t)worker * ((int64_t)a.d * a.n + (SLICED ? 0 : 2 * a.d));
   dD += dpp_get<QUAD_XOR1>(dD);
   dD += dpp_get<QUAD_XOR2>(dD);
   dbias += dpp_get<QUAD_XOR1>(dbias);
@@ -587,11 +610,64 @@ __global__ __launch_bounds__(64 * bwd_waves(NP), NP <= 4 ? 2 : 1) void scan_bwd_
   if (!on) return;
 #pragma unroll
   for (int i = 0; i < NP; ++i)
-    if (q * NP + i < a.n) part[(int64_t)c * a.n + q * NP + i] = dA[i] * LN2;   // (it was summed up with delta log2 e)
-  if (q == 0) {
+    if (q * NP + i < n_here) part[(int64_t)c * a.n + n0 + q * NP + i] = dA[i] * LN2;   // (it was summed up with delta log2 e)
+  if (!SLICED && q == 0) {
     part[(int64_t)a.d * a.n + c] = dD;
     part[(int64_t)a.d * a.n + a.d + c] = dbias;
   }
+}
+
+// What is left of a row once the slices' sums over their states are there: a thread has a column, a workgroup walks over pieces of 8
+// events (of 32, 10,000 events of 86 columns took 31 us); dD and dbias per workgroup.
+template <class T>
+__global__ __launch_bounds__(256) void scan_finish_kernel(ScanArgs a, int per_x, int col_tiles) {
+  __shared__ float acc[2][256];
+  const int tx = threadIdx.x % per_x, ty = threadIdx.x / per_x, per_y = 256 / per_x;
+  const int tile = blockIdx.x % col_tiles, worker = blockIdx.x / col_tiles, workers = gridDim.x / col_tiles;
+  const int col = tile * per_x + tx, c = min(col, a.d - 1);
+  const bool on = col < a.d;
+  const float bias = a.bias ? a.bias[c] : 0.0f, D = a.D ? a.D[c] : 0.0f;
+  const int64_t per_slice = a.q.n_rows * a.d, per_kind = a.slices * per_slice;
+  float dD = 0.0f, dbias = 0.0f;
+  for (int64_t item = worker; item < a.items; item += workers) {
+    const Piece p = piece_at(a.q, (int)item, FINISH_BITS);
+    if (p.none) continue;
+    for (int t = p.t0 + ty; on && t < p.t1; t += per_y) {
+      const int64_t row = seq_row(a.q, p.r, t);
+      float y0 = 0.0f, s1 = 0.0f, s2 = 0.0f;
+      for (int k = 0; k < a.slices; ++k) {
+        const float* o = a.part_y + k * per_slice + row * a.d + c;
+        y0 += o[0];
+        s1 += o[per_kind];
+        s2 += o[2 * per_kind];
+      }
+      const float x = (float)(static_cast<const T*>(a.x) + row * a.ld_x)[c], raw = (float)(static_cast<const T*>(a.dt) + row * a.ld_dt)[c] + bias;
+      const float dy = (float)(static_cast<const T*>(a.dy) + row * a.ld_dy)[c], delta = a.softplus ? softplus(raw) : raw;
+      float gy = dy;
+      if (a.z) {
+        const float z = (float)(static_cast<const T*>(a.z) + row * a.ld_z)[c], sg = sigmoid(z);
+        gy = dy * z * sg;
+        (static_cast<T*>(a.dz) + row * a.ld_dz)[c] = (T)(dy * fmaf(D, x, y0) * (sg * fmaf(z, 1.0f - sg, 1.0f)));
+      }
+      const float dd = fmaf(x, s1, s2), draw = a.softplus ? dd * sigmoid(raw) : dd;
+      (static_cast<T*>(a.dx) + row * a.ld_dx)[c] = (T)fmaf(D, gy, delta * s1);
+      (static_cast<T*>(a.ddt) + row * a.ld_ddt)[c] = (T)draw;
+      dD = fmaf(gy, x, dD);
+      dbias += draw;
+    }
+  }
+  if (a.part == nullptr) return;
+  acc[0][threadIdx.x] = dD;
+  acc[1][threadIdx.x] = dbias;
+  __syncthreads();
+  if (ty != 0 || !on) return;
+  for (int r = 1; r < per_y; ++r) {
+    dD += acc[0][r * per_x + tx];
+    dbias += acc[1][r * per_x + tx];
+  }
+  float* part = a.part + (int64_t)worker * 2 * a.d;
+  part[c] = dD;
+  part[a.d + c] = dbias;
 }
 
 // dB and dC of the rows of sequences: the column tiles' parts in order
@@ -857,36 +933,41 @@ template <int MODE> static int scan_forward(ScanArgs a, hipStream_t s, int dtype
 constexpr int BWD_SPREAD = 256, BWD_FILL = 5;   // workgroups: one, and five, to a compute unit
 constexpr int BWD_WORKERS = 1024;   // at most as many partial sums of the weights' gradients
 
-struct BwdPlan { int np, tiles, bits, workers; int64_t items; };
+struct BwdPlan { int tiles, slices, bits, workers, finish_x, finish_tiles, finishers; int64_t items; };
 static BwdPlan bwd_plan(const tgnn_seqs& q, int d, int n, int groups) {
-  BwdPlan p;
-  p.np = n <= 4 ? 1 : n <= 8 ? 2 : n <= 16 ? 4 : n <= 32 ? 8 : 16;
-  const int cols = 16 * bwd_waves(p.np), dg = d / groups;
-  p.tiles = (dg + cols - 1) / cols;
-  const int64_t all = (int64_t)groups * p.tiles;
+  BwdPlan p = {};
+  const int dg = d / groups;
+  p.tiles = (dg + BWD_COLS - 1) / BWD_COLS;
+  p.slices = (n + SLICE - 1) / SLICE;
+  const int64_t all = (int64_t)groups * p.tiles * p.slices;
   p.bits = scan_segment(q, all, BWD_SPREAD, BWD_FILL);
   p.items = p.bits != WHOLE ? seg_total(q, p.bits) : q.n_seqs;
   p.workers = (int)std::max<int64_t>(1, std::min<int64_t>(p.items, std::min<int64_t>(BWD_WORKERS, 2 * BWD_SPREAD * BWD_FILL / all)));
+  for (p.finish_x = 1; p.finish_x < 256 && p.finish_x < d;) p.finish_x *= 2;
+  p.finish_tiles = (d + p.finish_x - 1) / p.finish_x;
+  p.finishers = (int)std::max<int64_t>(1, std::min<int64_t>(seg_total(q, FINISH_BITS), 2048 / p.finish_tiles));
   return p;
 }
-static int64_t bwd_bytes(const tgnn_seqs& q, int d, int n, int groups, bool saved, ScanArgs* a, void* ws, ScanArgs* fwd) {
+struct BwdSpace { float *saved = nullptr, *part = nullptr, *part2 = nullptr, *part_y = nullptr, *part_bc = nullptr, *seg_state = nullptr, *seg_delta = nullptr; };
+// Bytes of a backward call's workspace, and where its parts are; fwd: of the forward pass that forms the states (saved == false)
+static int64_t bwd_bytes(const tgnn_seqs& q, int d, int n, int groups, bool saved, BwdSpace* s, void* ws, ScanArgs* fwd) {
   const BwdPlan p = bwd_plan(q, d, n, groups);
+  BwdSpace none;
+  if (s == nullptr) s = &none;
   Take t{static_cast<char*>(ws)};
-  if (!saved) {   // the states are formed here
-    float* sv = t.floats(seg_total(q, CHUNK_BITS) * d * n);
-    if (a) a->saved = fwd->saved = sv;
-    const int64_t bytes = fwd_bytes(q, d, n, groups, fwd, ws ? static_cast<char*>(ws) + t.off : nullptr);
-    t.off += bytes;
+  if (!saved) {
+    s->saved = t.floats(seg_total(q, CHUNK_BITS) * d * n);
+    t.off += fwd_bytes(q, d, n, groups, fwd, ws ? static_cast<char*>(ws) + t.off : nullptr);
   }
   if (p.bits != WHOLE) {
-    float *st = t.floats(seg_total(q, p.bits) * d * n), *dl = t.floats(seg_total(q, p.bits) * d);
-    if (a) { a->seg_state = st; a->seg_delta = dl; }
+    s->seg_state = t.floats(seg_total(q, p.bits) * d * n);
+    s->seg_delta = t.floats(seg_total(q, p.bits) * d);
   }
-  float* part = t.floats((int64_t)p.workers * ((int64_t)d * n + 2 * d));
-  if (a) a->part = part;
-  if (p.tiles > 1) {
-    float* bc = t.floats((int64_t)p.tiles * q.n_rows * 2 * groups * n);
-    if (a) a->part_bc = bc;
+  s->part = t.floats((int64_t)p.workers * ((int64_t)d * n + 2 * d));
+  if (p.tiles > 1) s->part_bc = t.floats((int64_t)p.tiles * q.n_rows * 2 * groups * n);
+  if (p.slices > 1) {
+    s->part2 = t.floats((int64_t)p.finishers * 2 * d);
+    s->part_y = t.floats((int64_t)3 * p.slices * q.n_rows * d);
   }
   return t.off;
 }
@@ -1009,19 +1090,21 @@ extern "C" int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_sca
     return set_error(TGNN_E_WORKSPACE, "saved has %lld bytes, %lld are needed", (long long)saved_bytes,
                      (long long)tgnn_selective_scan_saved_bytes(seqs, d, scan->n_state));
   ScanArgs a = scan_args(seqs, scan), fwd = a;
-  const int64_t need = bwd_bytes(*seqs, d, a.n, a.groups, saved != nullptr, &a, workspace, &fwd);
+  BwdSpace space;
+  const int64_t need = bwd_bytes(*seqs, d, a.n, a.groups, saved != nullptr, &space, workspace, &fwd);
   if (int rc = check_workspace(workspace, workspace_bytes, need)) return rc;
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const BwdPlan plan = bwd_plan(*seqs, d, a.n, a.groups);
-  if (saved != nullptr) a.saved = const_cast<float*>(saved);
-  else if (seqs->n_seqs > 0)
+  a.saved = saved != nullptr ? const_cast<float*>(saved) : space.saved;
+  fwd.saved = a.saved;
+  if (saved == nullptr && seqs->n_seqs > 0)
     if (int rc = scan_forward<SCAN_STATES>(fwd, s, scan->dtype)) return rc;
   a.dy = dy; a.ld_dy = ld_dy;
   a.dx = grads->dx; a.ddt = grads->ddt; a.dz = grads->dz; a.dB = grads->dB; a.dC = grads->dC;
   a.ld_dx = grads->ld_dx; a.ld_ddt = grads->ld_ddt; a.ld_dz = grads->ld_dz; a.ld_db = grads->ld_db; a.ld_dc = grads->ld_dc;
-  a.bits = plan.bits; a.items = plan.items;
-  const bool weights = grads->dA != nullptr || grads->dD != nullptr || grads->ddt_bias != nullptr;
-  if (!weights) a.part = nullptr;
+  a.seg_state = space.seg_state; a.seg_delta = space.seg_delta; a.part_bc = space.part_bc; a.part_y = space.part_y;
+  a.bits = plan.bits; a.items = plan.items; a.slices = plan.slices;
+  const bool weights = grads->dA != nullptr || grads->dD != nullptr || grads->ddt_bias != nullptr, sliced = plan.slices > 1;
   if (seqs->n_seqs > 0) {
     unsigned chain = 0, back = 0, sum = 0;
     const int64_t waves = plan.items * a.groups * fwd_tiles(a.dg);
@@ -1032,23 +1115,37 @@ extern "C" int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_sca
     if (int rc = launch_grid(seg_total(*seqs, SUM_BITS), &sum)) return rc;
     scan_shape(scan->dtype, a.n, [&](auto t, auto np) {
       using T = decltype(t);
-      constexpr int NP = decltype(np)::value;
+      constexpr int NP = decltype(np)::value, LANE = NP < SLICE ? NP / 4 : SLICE / 4;
+      constexpr bool SLICED = NP > SLICE;
       if (plan.bits != WHOLE) {
         a.tiles = fwd_tiles(a.dg);
         launch_scan<T, NP, SCAN_BACK_PART>(a, dim3((unsigned)((waves + 3) / 4)), s);
         launch_chain<true>(a, chain, s);
       }
       a.tiles = plan.tiles;
-      const dim3 grid((unsigned)(plan.workers * a.groups * plan.tiles)), block(64 * bwd_waves(NP / 4));
-      if (a.softplus && a.z != nullptr) hipLaunchKernelGGL((scan_bwd_kernel<T, NP / 4, true>), grid, block, 0, s, a);
-      else hipLaunchKernelGGL((scan_bwd_kernel<T, NP / 4, false>), grid, block, 0, s, a);
+      a.part = weights ? space.part : nullptr;
+      const dim3 grid((unsigned)(plan.workers * a.groups * plan.tiles * plan.slices)), block(64 * BWD_WAVES);
+      if (a.softplus && a.z != nullptr) hipLaunchKernelGGL((scan_bwd_kernel<T, LANE, true, SLICED>), grid, block, 0, s, a);
+      else hipLaunchKernelGGL((scan_bwd_kernel<T, LANE, false, SLICED>), grid, block, 0, s, a);
       if (a.part_bc) hipLaunchKernelGGL((scan_bc_sum_kernel<T>), dim3(sum), dim3(256), 0, s, a);
+      if constexpr (SLICED) {
+        a.items = seg_total(*seqs, FINISH_BITS);
+        a.part = weights ? space.part2 : nullptr;
+        hipLaunchKernelGGL((scan_finish_kernel<T>), dim3((unsigned)(plan.finishers * plan.finish_tiles)), dim3(256), 0, s, a, plan.finish_x,
+                           plan.finish_tiles);
+      }
     });
     TGNN_LAUNCH_CHECK();
   }
   if (weights) {
     const int64_t dn = (int64_t)d * a.n;
-    column_sum(ColumnSum{a.part, seqs->n_seqs > 0 ? plan.workers : 0, dn + 2 * d, {grads->dA, grads->dD, grads->ddt_bias}, {dn, d, d}, accumulate}, s);
+    const int n_part = seqs->n_seqs > 0 ? plan.workers : 0, n_part2 = seqs->n_seqs > 0 ? plan.finishers : 0;
+    if (!sliced) {
+      column_sum(ColumnSum{space.part, n_part, dn + 2 * d, {grads->dA, grads->dD, grads->ddt_bias}, {dn, d, d}, accumulate}, s);
+    } else {
+      column_sum(ColumnSum{space.part, n_part, dn, {grads->dA, nullptr, nullptr}, {dn, 0, 0}, accumulate}, s);
+      column_sum(ColumnSum{space.part2, n_part2, 2 * (int64_t)d, {grads->dD, grads->ddt_bias, nullptr}, {d, d, 0}, accumulate}, s);
+    }
     TGNN_LAUNCH_CHECK();
   }
   return TGNN_OK;

@@ -142,6 +142,18 @@ def test_optional_parts(z, D, bias, softplus, state):
         compare(got, ref, names_of(t), "optional", q)
 
 
+@pytest.mark.parametrize("z,D,bias,softplus,state", [(0, 1, 1, 1, 1), (1, 0, 0, 1, 0), (0, 0, 0, 0, 1), (1, 1, 1, 0, 0)])
+@pytest.mark.parametrize("n", [17, 47, 64])
+def test_many_states(n, z, D, bias, softplus, state):
+    """More states than a workgroup of the backward pass takes at once: their sums are joined; several column tiles, padding."""
+    from paper_2307_07649_amd import tgnn
+    for q in (lists([5, 0, 6, 1, 3], 6), packed([90, 3, 0, 40], behind=3)):
+        t, dy = inputs(q, 142, n, 2, "f32", n, z=z, D=D, bias=bias, softplus=bool(softplus), state=state)
+        got = run(tgnn, q, t, dy, softplus=bool(softplus))
+        compare(got, ref_of(q, t, dy, 2, softplus=bool(softplus)), names_of(t), f"{n} states", q)
+        check_rows_outside(q, got, ["y", "dx", "ddt", "dB", "dC"] + ["dz"] * z)
+
+
 def test_many_short_lists():
     """More pieces than workgroups, several column tiles: every one of the partial sums is used."""
     from paper_2307_07649_amd import tgnn
