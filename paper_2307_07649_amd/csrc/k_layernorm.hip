@@ -272,7 +272,11 @@ template <int V, class F> static bool norm_shape(int64_t packs, F f) {
   TGNN_NORM_SHAPE(16, 2)
   TGNN_NORM_SHAPE(64, 1)
   TGNN_NORM_SHAPE(64, 2)
-  TGNN_NORM_SHAPE(64, 4)
+  if constexpr (V == 4) {
+    TGNN_NORM_SHAPE(64, 4)
+  } else {
+    TGNN_NORM_SHAPE(256, 1)
+  }
   TGNN_NORM_SHAPE(256, 2)
   TGNN_NORM_SHAPE(512, 2)
   if constexpr (V == 4) {
