@@ -375,9 +375,10 @@ int32_t tgnn_profile_read(tgnn_ctx* ctx, int32_t stage, int32_t* out_count, doub
  * captured into a graph.  Where one needs scratch memory the caller hands it over (workspace, 16-byte aligned,
  * tgnn_..._workspace_bytes; what it holds before and after does not matter; two calls that may overlap in time need two).
  * Row arrays (x, y, dy, ...) hold float, bfloat16 or float16 values (`dtype`, one type for all row arrays of a call), start at any
- * multiple of the value's size and have their rows `ld_...` values apart; weights, states and their gradients are float and
+ * multiple of the value's size and have their rows `ld_...` values apart (of the convolution's and the scan's: at most 2^27); weights, states and their gradients are float and
  * contiguous.  Arithmetic is in float, sums over many rows in double at the end, and no sum depends on the order in which
- * workgroups finish.  Gradients of weights are added to what is there (accumulate != 0) or written (0); NULL: not wanted. */
+ * workgroups finish.  What a call writes (states, saved values, the workspace, weights' gradients too) shares memory with nothing else of
+ * the call, except where a function says so.  Gradients of weights are added to what is there (accumulate != 0) or written (0); NULL: not wanted. */
 #define TGNN_F32 0
 #define TGNN_BF16 1
 #define TGNN_F16 2
@@ -456,7 +457,7 @@ int32_t tgnn_selective_scan_fwd(const tgnn_seqs* seqs, const tgnn_scan* scan, vo
                                 int64_t saved_bytes, void* workspace, int64_t workspace_bytes, void* stream);
 /* One event for each of n_rows sequences; state_out may be scan->state_in. */
 int32_t tgnn_selective_scan_step(const tgnn_scan* scan, int64_t n_rows, void* y, int64_t ld_y, float* state_out, void* stream);
-/* Gradients for dy; the inputs as in the forward call.  saved NULL: the states are formed again.  No gradient array may overlap an input.  The gradient
+/* Gradients for dy; the inputs as in the forward call.  saved NULL: the states are formed again.  No gradient array may overlap an input or another one.  The gradient
  * of a row's step size is that of dt (through the softplus), ddt_bias is its sum over all rows of sequences. */
 int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_scan* scan, const void* dy, int64_t ld_dy, const float* saved,
                                 int64_t saved_bytes, const tgnn_scan_grads* grads, int32_t accumulate, void* workspace,

@@ -93,8 +93,11 @@ __device__ __forceinline__ int64_t state_of(const int32_t* idx, int n_states, in
 template <class T, int V, int W, bool WIDE, bool ANY>
 __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
   const int per_y = 256 / a.per_x, col_tiles = (a.d + a.per_x * V - 1) / (a.per_x * V);
-  const int c = ((int)(blockIdx.x % col_tiles) * a.per_x + (int)threadIdx.x % a.per_x) * V;
-  const int item0 = (int)(blockIdx.x / col_tiles) * per_y, item = item0 + (int)threadIdx.x / a.per_x;
+  const unsigned number = group_number();
+  const int c = ((int)(number % col_tiles) * a.per_x + (int)threadIdx.x % a.per_x) * V;
+  const int64_t first = (int64_t)(number / col_tiles) * per_y;
+  if (first >= a.items) return;
+  const int item0 = (int)first, item = item0 + (int)threadIdx.x / a.per_x;
   const int s0 = seg_find(a.q, item0, a.bits);
   if (c >= a.d || item >= a.items) return;
   const int at = WIDE ? __builtin_amdgcn_readfirstlane(item) : item;
@@ -161,7 +164,7 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
 template <class T, int V, int W, bool ANY>
 __global__ __launch_bounds__(256) void conv_step_kernel(ConvArgs a) {
   const int packs = (a.d + V - 1) / V;
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = (int64_t)group_number() * 256 + threadIdx.x;
   if (i >= a.items * packs) return;
   const int64_t row = i / packs;
   const int c = (int)(i - row * packs) * V;
@@ -410,10 +413,10 @@ int check_row_array(const char* name, const void* p, int64_t ld, int64_t rows, i
 
 using namespace tgnn;
 
-static int conv_grid(int64_t groups, int col_tiles, unsigned* out) {
+static int conv_grid(int64_t groups, int col_tiles, dim3* out) {
   const int64_t n = groups * col_tiles;
   if (n > INT_MAX) return set_error(TGNN_E_OUT_OF_RANGE, "%lld workgroups", (long long)n);
-  *out = (unsigned)n;
+  *out = group_grid(n);
   return TGNN_OK;
 }
 
@@ -428,7 +431,7 @@ extern "C" int32_t tgnn_causal_conv_fwd(const tgnn_seqs* seqs, int32_t dtype, in
   if (!aligned_to(state_in, size) || !aligned_to(state_out, size)) return set_error(TGNN_E_MISALIGNED, "a state is not aligned to its type");
   const size_t state_bytes = (size_t)n_states * (width - 1) * d * size;
   if (spans_overlap(state_in, state_bytes, state_out, state_bytes)) return set_error(TGNN_E_INVALID_ARG, "state_out overlaps state_in");
-  if (spans_overlap(x, rows_span(seqs->n_rows, d, ld_x, size), y, rows_span(seqs->n_rows, d, ld_y, size)))
+  if (rows_overlap(seqs->n_rows, size, {x, d, ld_x}, {y, d, ld_y}))
     return set_error(TGNN_E_INVALID_ARG, "y overlaps x");
   if (seqs->n_seqs == 0) return TGNN_OK;
   ConvArgs a = {};
@@ -446,11 +449,11 @@ extern "C" int32_t tgnn_causal_conv_fwd(const tgnn_seqs* seqs, int32_t dtype, in
     a.items = seg_total(*seqs, a.bits);
     a.per_x = conv_columns(d, V);
     const int per_y = 256 / a.per_x, tiles = (d + a.per_x * V - 1) / (a.per_x * V);
-    unsigned grid;
+    dim3 grid;
     rc = conv_grid((a.items + per_y - 1) / per_y, tiles, &grid);
     if (rc != TGNN_OK) return;
-    if (a.per_x >= 64) hipLaunchKernelGGL((conv_fwd_kernel<T, V, W, true, ANY>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
-    else hipLaunchKernelGGL((conv_fwd_kernel<T, V, W, false, ANY>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    if (a.per_x >= 64) hipLaunchKernelGGL((conv_fwd_kernel<T, V, W, true, ANY>), grid, dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    else hipLaunchKernelGGL((conv_fwd_kernel<T, V, W, false, ANY>), grid, dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
   });
   if (rc != TGNN_OK) return rc;
   TGNN_LAUNCH_CHECK();
@@ -469,7 +472,7 @@ extern "C" int32_t tgnn_causal_conv_step(int32_t dtype, int64_t n_rows, int32_t 
   const size_t state_bytes = (size_t)n_states * (width - 1) * d * size;
   if (state_in != state_out && spans_overlap(state_in, state_bytes, state_out, state_bytes))
     return set_error(TGNN_E_INVALID_ARG, "state_out overlaps state_in without being it");
-  if (!(x == y && ld_x == ld_y) && spans_overlap(x, rows_span(n_rows, d, ld_x, size), y, rows_span(n_rows, d, ld_y, size)))
+  if (!(x == y && ld_x == ld_y) && rows_overlap(n_rows, size, {x, d, ld_x}, {y, d, ld_y}))
     return set_error(TGNN_E_INVALID_ARG, "y overlaps x without being it");
   if (n_rows == 0) return TGNN_OK;
   ConvArgs a = {};
@@ -483,9 +486,9 @@ extern "C" int32_t tgnn_causal_conv_step(int32_t dtype, int64_t n_rows, int32_t 
   conv_shape<false>(dtype, width, d, n_rows, p, ld, 4, [&](auto t, auto v, auto wd, auto any) {
     using T = decltype(t);
     constexpr int V = decltype(v)::value, W = decltype(wd)::value;
-    unsigned grid;
+    dim3 grid;
     rc = conv_grid((n_rows * ((d + V - 1) / V) + 255) / 256, 1, &grid);
-    if (rc == TGNN_OK) hipLaunchKernelGGL((conv_step_kernel<T, V, W, decltype(any)::value>), dim3(grid), dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
+    if (rc == TGNN_OK) hipLaunchKernelGGL((conv_step_kernel<T, V, W, decltype(any)::value>), grid, dim3(256), 0, reinterpret_cast<hipStream_t>(stream), a);
   });
   if (rc != TGNN_OK) return rc;
   TGNN_LAUNCH_CHECK();
@@ -509,8 +512,7 @@ extern "C" int32_t tgnn_causal_conv_bwd(const tgnn_seqs* seqs, int32_t dtype, in
   if (!aligned_to(state_in, type_size(dtype)) || !aligned_to(d_weight, 4) || !aligned_to(d_bias, 4))
     return set_error(TGNN_E_MISALIGNED, "state_in, d_weight or d_bias is not aligned to its type");
   const int size = type_size(dtype);
-  const size_t span = rows_span(seqs->n_rows, d, ld_dx, size);
-  if (spans_overlap(dx, span, x, rows_span(seqs->n_rows, d, ld_x, size)) || spans_overlap(dx, span, dy, rows_span(seqs->n_rows, d, ld_dy, size)))
+  if (rows_overlap(seqs->n_rows, size, {dx, d, ld_dx}, {x, d, ld_x}) || rows_overlap(seqs->n_rows, size, {dx, d, ld_dx}, {dy, d, ld_dy}))
     return set_error(TGNN_E_INVALID_ARG, "dx overlaps x or dy");
   const bool weights = d_weight != nullptr || d_bias != nullptr;
   if (weights) {

@@ -324,7 +324,7 @@ extern "C" int32_t tgnn_layer_norm_fwd(int32_t dtype, int64_t n_rows, int32_t n_
   if (int rc = check_floats("out_rstd", out_rstd, false)) return rc;
   if (!(eps >= 0.0f)) return set_error(TGNN_E_INVALID_ARG, "eps = %g: a number that is not negative is needed", (double)eps);
   const int size = type_size(dtype);
-  if (!(x == y && ld_x == ld_y) && spans_overlap(x, rows_span(n_rows, n_cols, ld_x, size), y, rows_span(n_rows, n_cols, ld_y, size)))
+  if (!(x == y && ld_x == ld_y) && rows_overlap(n_rows, size, {x, n_cols, ld_x}, {y, n_cols, ld_y}))
     return set_error(TGNN_E_INVALID_ARG, "y overlaps x without being it");
   if (n_rows == 0) return TGNN_OK;
   NormArgs a = {};
@@ -368,10 +368,9 @@ extern "C" int32_t tgnn_layer_norm_bwd(int32_t dtype, int64_t n_rows, int32_t n_
   if (int rc = check_floats("d_weight", d_weight, false)) return rc;
   if (int rc = check_floats("d_bias", d_bias, false)) return rc;
   const int size = type_size(dtype);
-  const size_t span = rows_span(n_rows, n_cols, ld_dx, size);
-  if (!(dy == dx && ld_dy == ld_dx) && spans_overlap(dy, rows_span(n_rows, n_cols, ld_dy, size), dx, span))
+  if (!(dy == dx && ld_dy == ld_dx) && rows_overlap(n_rows, size, {dy, n_cols, ld_dy}, {dx, n_cols, ld_dx}))
     return set_error(TGNN_E_INVALID_ARG, "dx overlaps dy without being it");
-  if (spans_overlap(x, rows_span(n_rows, n_cols, ld_x, size), dx, span)) return set_error(TGNN_E_INVALID_ARG, "dx overlaps x");
+  if (rows_overlap(n_rows, size, {x, n_cols, ld_x}, {dx, n_cols, ld_dx})) return set_error(TGNN_E_INVALID_ARG, "dx overlaps x");
   const bool weights = d_weight != nullptr || d_bias != nullptr;
   if (weights) {
     if (workspace == nullptr) return set_error(TGNN_E_NULL_PTR, "workspace is NULL");

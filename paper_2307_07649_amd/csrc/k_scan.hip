@@ -130,7 +130,7 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a) {
   using E = Events<T, NP>;
   constexpr bool BACK = MODE == SCAN_BACK_PART, OUT = MODE == SCAN_Y, NEED_B = !BACK, NEED_C = OUT || BACK, PART = MODE == SCAN_PART || BACK;
   __shared__ float stage[4][2][4 * NP];
-  const unsigned w4 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wave = blockIdx.x * 4 + w4;
+  const unsigned w4 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, wave = group_number() * 4 + w4;
   const unsigned all = (unsigned)(a.groups * a.tiles), item = wave / all, tile = wave - item * all;
   if (item >= a.items) return;
   const Piece p = piece_at(a.q, (int)item, a.bits);
@@ -262,8 +262,10 @@ __global__ __launch_bounds__(256) void scan_chain_kernel(ScanArgs a) {
   constexpr int COLS = 256 / RUNS;
   __shared__ float part[RUNS][COLS], sum[RUNS][COLS];
   const int64_t dn = (int64_t)a.d * a.n, per = (dn + COLS - 1) / COLS;
-  const int s = (int)(blockIdx.x / per), x = threadIdx.x % COLS, run = threadIdx.x / COLS;
-  const int64_t e = (blockIdx.x - s * per) * COLS + x;
+  const int64_t number = group_number();
+  const int s = (int)(number / per), x = threadIdx.x % COLS, run = threadIdx.x / COLS;
+  if (s >= a.q.n_seqs) return;
+  const int64_t e = (number - s * per) * COLS + x;
   const bool on = e < dn;
   const int c = on ? (int)(e / a.n) : 0;
   const Seq r = seq_at(a.q, s);
@@ -673,7 +675,9 @@ __global__ __launch_bounds__(256) void scan_finish_kernel(ScanArgs a, int per_x,
 // dB and dC of the rows of sequences: the column tiles' parts in order
 template <class T>
 __global__ __launch_bounds__(256) void scan_bc_sum_kernel(ScanArgs a) {
-  const Piece p = piece_at(a.q, (int)blockIdx.x, SUM_BITS);
+  const unsigned item = group_number();
+  if (item >= a.items) return;
+  const Piece p = piece_at(a.q, (int)item, SUM_BITS);
   if (p.none) return;
   const int per = a.groups * a.n;
   for (int i = threadIdx.x; i < (p.t1 - p.t0) * 2 * per; i += 256) {
@@ -693,8 +697,10 @@ __global__ __launch_bounds__(256) void scan_bc_sum_kernel(ScanArgs a) {
 // on their way, 65 (138 registers, half the wavefronts).
 template <class T, bool QUAD>
 __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int bits, int tiles) {
-  const int tile = blockIdx.x % tiles, part = threadIdx.x & ((1 << bits) - 1), q = threadIdx.x & 3;
-  const int64_t row0 = (int64_t)(blockIdx.x / tiles) * 4, last = a.items - 1;
+  const unsigned number = group_number();
+  const int tile = number % tiles, part = threadIdx.x & ((1 << bits) - 1), q = threadIdx.x & 3;
+  const int64_t row0 = (int64_t)(number / tiles) * 4, last = a.items - 1;
+  if (row0 > last) return;
   const int col = tile * (256 >> bits) + (int)(threadIdx.x >> bits), c = min(col, a.d - 1), n0 = part * 4;
   const bool on = col < a.d, whole = n0 + 4 <= a.n;
   const int s0 = min(n0, a.n - 1), bc = c / a.dg * a.n + s0;   // (lanes without a state read another's)
@@ -883,21 +889,21 @@ static int64_t fwd_bytes(const tgnn_seqs& q, int d, int n, int groups, ScanArgs*
   return t.off;
 }
 
-static int launch_grid(int64_t n, unsigned* out) {
+static int launch_grid(int64_t n, dim3* out) {
   if (n > INT_MAX) return set_error(TGNN_E_OUT_OF_RANGE, "%lld workgroups", (long long)n);
-  *out = (unsigned)n;
+  *out = group_grid(n);
   return TGNN_OK;
 }
 
 // Runs from 64 segments of the longest sequence on
 static bool chain_runs(const ScanArgs& a) { return std::min<int64_t>(a.q.max_len, scan_rows(a.q)) > int64_t(64) << a.bits; }
-static int chain_grid(const ScanArgs& a, unsigned* out) {
+static int chain_grid(const ScanArgs& a, dim3* out) {
   const int cols = chain_runs(a) ? 32 : 256;
   return launch_grid(a.q.n_seqs * (((int64_t)a.d * a.n + cols - 1) / cols), out);
 }
-template <bool BACK> static void launch_chain(const ScanArgs& a, unsigned grid, hipStream_t s) {
-  if (chain_runs(a)) hipLaunchKernelGGL((scan_chain_kernel<BACK, 8>), dim3(grid), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((scan_chain_kernel<BACK, 1>), dim3(grid), dim3(256), 0, s, a);
+template <bool BACK> static void launch_chain(const ScanArgs& a, dim3 grid, hipStream_t s) {
+  if (chain_runs(a)) hipLaunchKernelGGL((scan_chain_kernel<BACK, 8>), grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((scan_chain_kernel<BACK, 1>), grid, dim3(256), 0, s, a);
 }
 
 template <class T, int NP, int MODE> static void launch_scan(const ScanArgs& a, dim3 grid, hipStream_t s) {
@@ -913,8 +919,8 @@ template <int MODE> static int scan_forward(ScanArgs a, hipStream_t s, int dtype
   a.items = a.bits != WHOLE ? seg_total(a.q, a.bits) : a.q.n_seqs;
   const int64_t waves = a.items * a.groups * a.tiles;
   if (waves > INT_MAX) return set_error(TGNN_E_OUT_OF_RANGE, "%lld wavefronts", (long long)waves);
-  const dim3 grid((unsigned)((waves + 3) / 4));
-  unsigned chain = 0;
+  const dim3 grid = group_grid((waves + 3) / 4);
+  dim3 chain;
   if (a.bits != WHOLE)
     if (int rc = chain_grid(a, &chain)) return rc;
   scan_shape(dtype, a.n, [&](auto t, auto np) {
@@ -1017,11 +1023,9 @@ extern "C" int32_t tgnn_selective_scan_fwd(const tgnn_seqs* seqs, const tgnn_sca
   if (spans_overlap(scan->state_in, states, state_out, states)) return set_error(TGNN_E_INVALID_ARG, "state_out overlaps state_in");
   const int size = type_size(scan->dtype), bc = scan->n_groups * scan->n_state;
   const int64_t rows = seqs->n_rows;
-  const size_t span = rows_span(rows, scan->d, ld_y, size);
-  if (spans_overlap(y, span, scan->x, rows_span(rows, scan->d, scan->ld_x, size)) || spans_overlap(y, span, scan->dt, rows_span(rows, scan->d, scan->ld_dt, size)) ||
-      spans_overlap(y, span, scan->z, rows_span(rows, scan->d, scan->ld_z, size)) || spans_overlap(y, span, scan->B, rows_span(rows, bc, scan->ld_b, size)) ||
-      spans_overlap(y, span, scan->C, rows_span(rows, bc, scan->ld_c, size)))
-    return set_error(TGNN_E_INVALID_ARG, "y overlaps an input");
+  for (const RowArray& in : {RowArray{scan->x, scan->d, scan->ld_x}, RowArray{scan->dt, scan->d, scan->ld_dt}, RowArray{scan->z, scan->d, scan->ld_z},
+                             RowArray{scan->B, bc, scan->ld_b}, RowArray{scan->C, bc, scan->ld_c}})
+    if (rows_overlap(rows, size, {y, scan->d, ld_y}, in)) return set_error(TGNN_E_INVALID_ARG, "y overlaps an input");
   ScanArgs a = scan_args(seqs, scan);
   const int64_t need = fwd_bytes(*seqs, a.d, a.n, a.groups, &a, workspace);
   if (int rc = check_workspace(workspace, workspace_bytes, need)) return rc;
@@ -1039,24 +1043,22 @@ extern "C" int32_t tgnn_selective_scan_step(const tgnn_scan* scan, int64_t n_row
   if (scan->state_in != state_out && spans_overlap(scan->state_in, states, state_out, states))
     return set_error(TGNN_E_INVALID_ARG, "state_out overlaps state_in without being it");
   const int size = type_size(scan->dtype), bc = scan->n_groups * scan->n_state;
-  const size_t span = rows_span(n_rows, scan->d, ld_y, size);
-  if (spans_overlap(y, span, scan->x, rows_span(n_rows, scan->d, scan->ld_x, size)) || spans_overlap(y, span, scan->dt, rows_span(n_rows, scan->d, scan->ld_dt, size)) ||
-      spans_overlap(y, span, scan->z, rows_span(n_rows, scan->d, scan->ld_z, size)) || spans_overlap(y, span, scan->B, rows_span(n_rows, bc, scan->ld_b, size)) ||
-      spans_overlap(y, span, scan->C, rows_span(n_rows, bc, scan->ld_c, size)))
-    return set_error(TGNN_E_INVALID_ARG, "y overlaps an input");
+  for (const RowArray& in : {RowArray{scan->x, scan->d, scan->ld_x}, RowArray{scan->dt, scan->d, scan->ld_dt}, RowArray{scan->z, scan->d, scan->ld_z},
+                             RowArray{scan->B, bc, scan->ld_b}, RowArray{scan->C, bc, scan->ld_c}})
+    if (rows_overlap(n_rows, size, {y, scan->d, ld_y}, in)) return set_error(TGNN_E_INVALID_ARG, "y overlaps an input");
   if (n_rows == 0) return TGNN_OK;
   ScanArgs a = scan_args(nullptr, scan);
   a.y = y; a.ld_y = ld_y; a.state_out = state_out; a.items = n_rows;
   int bits = 0;
   while ((4 << bits) < a.n) ++bits;
   const int tiles = (a.d + (256 >> bits) - 1) / (256 >> bits);
-  unsigned grid;
+  dim3 grid;
   if (int rc = launch_grid((n_rows + 3) / 4 * tiles, &grid)) return rc;
   with_type(scan->dtype, [&](auto t) {
     using T = decltype(t);
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (bits >= 2) hipLaunchKernelGGL((scan_step_kernel<T, true>), dim3(grid), dim3(256), 0, s, a, bits, tiles);
-    else hipLaunchKernelGGL((scan_step_kernel<T, false>), dim3(grid), dim3(256), 0, s, a, bits, tiles);
+    if (bits >= 2) hipLaunchKernelGGL((scan_step_kernel<T, true>), grid, dim3(256), 0, s, a, bits, tiles);
+    else hipLaunchKernelGGL((scan_step_kernel<T, false>), grid, dim3(256), 0, s, a, bits, tiles);
   });
   TGNN_LAUNCH_CHECK();
   return TGNN_OK;
@@ -1070,18 +1072,17 @@ extern "C" int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_sca
   if (int rc = check_scan(scan, rows)) return rc;
   if (grads == nullptr) return set_error(TGNN_E_NULL_PTR, "grads is NULL");
   const int d = scan->d, bc = scan->n_groups * scan->n_state, size = type_size(scan->dtype);
-  struct Rows { const char* name; const void* p; int64_t ld; int cols; };
-  const Rows out[] = {{"dx", grads->dx, grads->ld_dx, d}, {"ddt", grads->ddt, grads->ld_ddt, d}, {"dB", grads->dB, grads->ld_db, bc},
-                      {"dC", grads->dC, grads->ld_dc, bc}, {"dz", grads->dz, grads->ld_dz, d}};
-  const Rows in[] = {{"dy", dy, ld_dy, d}, {"x", scan->x, scan->ld_x, d}, {"dt", scan->dt, scan->ld_dt, d}, {"B", scan->B, scan->ld_b, bc},
-                     {"C", scan->C, scan->ld_c, bc}, {"z", scan->z, scan->ld_z, d}};
+  struct Named { const char* name; RowArray a; };
+  const Named out[] = {{"dx", {grads->dx, d, grads->ld_dx}}, {"ddt", {grads->ddt, d, grads->ld_ddt}}, {"dB", {grads->dB, bc, grads->ld_db}},
+                       {"dC", {grads->dC, bc, grads->ld_dc}}, {"dz", {grads->dz, d, grads->ld_dz}}};
+  const Named in[] = {{"dy", {dy, d, ld_dy}}, {"x", {scan->x, d, scan->ld_x}}, {"dt", {scan->dt, d, scan->ld_dt}},
+                      {"B", {scan->B, bc, scan->ld_b}}, {"C", {scan->C, bc, scan->ld_c}}, {"z", {scan->z, d, scan->ld_z}}};
   if (int rc = check_row_array("dy", dy, ld_dy, rows, d, scan->dtype)) return rc;
   const int n_out = scan->z != nullptr ? 5 : 4;
   for (int i = 0; i < n_out; ++i) {
-    if (int rc = check_row_array(out[i].name, out[i].p, out[i].ld, rows, out[i].cols, scan->dtype)) return rc;
-    for (const Rows& r : in)
-      if (spans_overlap(out[i].p, rows_span(rows, out[i].cols, out[i].ld, size), r.p, rows_span(rows, r.cols, r.ld, size)))
-        return set_error(TGNN_E_INVALID_ARG, "%s overlaps %s", out[i].name, r.name);
+    if (int rc = check_row_array(out[i].name, out[i].a.p, out[i].a.ld, rows, (int)out[i].a.cols, scan->dtype)) return rc;
+    for (const Named& r : in)
+      if (rows_overlap(rows, size, out[i].a, r.a)) return set_error(TGNN_E_INVALID_ARG, "%s overlaps %s", out[i].name, r.name);
   }
   if (!aligned_to(grads->dA, 4) || !aligned_to(grads->dD, 4) || !aligned_to(grads->ddt_bias, 4))
     return set_error(TGNN_E_MISALIGNED, "dA, dD or ddt_bias is not aligned to its type");
@@ -1093,6 +1094,9 @@ extern "C" int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_sca
   BwdSpace space;
   const int64_t need = bwd_bytes(*seqs, d, a.n, a.groups, saved != nullptr, &space, workspace, &fwd);
   if (int rc = check_workspace(workspace, workspace_bytes, need)) return rc;
+  for (int i = 1; i < n_out; ++i)
+    for (int k = 0; k < i; ++k)
+      if (rows_overlap(rows, size, out[i].a, out[k].a)) return set_error(TGNN_E_INVALID_ARG, "%s overlaps %s", out[i].name, out[k].name);
   hipStream_t s = reinterpret_cast<hipStream_t>(stream);
   const BwdPlan plan = bwd_plan(*seqs, d, a.n, a.groups);
   a.saved = saved != nullptr ? const_cast<float*>(saved) : space.saved;
@@ -1106,20 +1110,22 @@ extern "C" int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_sca
   a.bits = plan.bits; a.items = plan.items; a.slices = plan.slices;
   const bool weights = grads->dA != nullptr || grads->dD != nullptr || grads->ddt_bias != nullptr, sliced = plan.slices > 1;
   if (seqs->n_seqs > 0) {
-    unsigned chain = 0, back = 0, sum = 0;
+    dim3 chain, back, sum;
     const int64_t waves = plan.items * a.groups * fwd_tiles(a.dg);
     if (plan.bits != WHOLE) {
       if (int rc = chain_grid(a, &chain)) return rc;
-      if (int rc = launch_grid(waves, &back)) return rc;
+      if (waves > INT_MAX) return set_error(TGNN_E_OUT_OF_RANGE, "%lld wavefronts", (long long)waves);
+      back = group_grid((waves + 3) / 4);
     }
-    if (int rc = launch_grid(seg_total(*seqs, SUM_BITS), &sum)) return rc;
+    const int64_t sums = seg_total(*seqs, SUM_BITS);
+    if (int rc = launch_grid(sums, &sum)) return rc;
     scan_shape(scan->dtype, a.n, [&](auto t, auto np) {
       using T = decltype(t);
       constexpr int NP = decltype(np)::value, LANE = NP < SLICE ? NP / 4 : SLICE / 4;
       constexpr bool SLICED = NP > SLICE;
       if (plan.bits != WHOLE) {
         a.tiles = fwd_tiles(a.dg);
-        launch_scan<T, NP, SCAN_BACK_PART>(a, dim3((unsigned)((waves + 3) / 4)), s);
+        launch_scan<T, NP, SCAN_BACK_PART>(a, back, s);
         launch_chain<true>(a, chain, s);
       }
       a.tiles = plan.tiles;
@@ -1127,7 +1133,10 @@ extern "C" int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_sca
       const dim3 grid((unsigned)(plan.workers * a.groups * plan.tiles * plan.slices)), block(64 * BWD_WAVES);
       if (a.softplus && a.z != nullptr) hipLaunchKernelGGL((scan_bwd_kernel<T, LANE, true, SLICED>), grid, block, 0, s, a);
       else hipLaunchKernelGGL((scan_bwd_kernel<T, LANE, false, SLICED>), grid, block, 0, s, a);
-      if (a.part_bc) hipLaunchKernelGGL((scan_bc_sum_kernel<T>), dim3(sum), dim3(256), 0, s, a);
+      if (a.part_bc) {
+        a.items = sums;
+        hipLaunchKernelGGL((scan_bc_sum_kernel<T>), sum, dim3(256), 0, s, a);
+      }
       if constexpr (SLICED) {
         a.items = seg_total(*seqs, FINISH_BITS);
         a.part = weights ? space.part2 : nullptr;

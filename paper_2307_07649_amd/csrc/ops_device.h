@@ -101,6 +101,24 @@ inline size_t rows_span(int64_t rows, int64_t cols, int64_t ld, int size) {
   return rows > 0 && cols > 0 ? ((size_t)(rows - 1) * ld + cols) * size : 0;
 }
 
+// Whether two row arrays of the same rows share memory; columns of one buffer that lie next to each other do not.
+struct RowArray { const void* p; int64_t cols, ld; };
+inline bool rows_overlap(int64_t rows, int size, const RowArray& a, const RowArray& b) {
+  if (!spans_overlap(a.p, rows_span(rows, a.cols, a.ld, size), b.p, rows_span(rows, b.cols, b.ld, size))) return false;
+  if (a.ld != b.ld) return true;
+  const uintptr_t pitch = (uintptr_t)a.ld * size, x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  const uintptr_t from = y >= x ? (y - x) % pitch : (pitch - (x - y) % pitch) % pitch;   // where b's columns begin in a's rows
+  return from < (uintptr_t)a.cols * size || from + (uintptr_t)b.cols * size > pitch;
+}
+
+// A launch of n workgroups of 256 threads, n <= INT_MAX: a grid has fewer than 2^32 threads along x, so that the workgroups of a larger one
+// are spread over y as well.  Some may lie behind the last one: a kernel has to look at its number.
+inline dim3 group_grid(int64_t n) {
+  constexpr int64_t ROW = 1 << 23;
+  return n <= ROW ? dim3((unsigned)n) : dim3((unsigned)ROW, (unsigned)((n + ROW - 1) / ROW));
+}
+__device__ __forceinline__ unsigned group_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 // ---- out[m] (+)= sum over p of part[p, m], for gradients of weights that many workgroups have parts of.  Columns
 // [0, c0) go to o0, [c0, c0 + c1) to o1, the next c2 to o2; the sums are taken in double and in one order.
 struct ColumnSum {

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from ops_common import TYPES, dev, f64, rng, wide_rows, within
+from ops_common import TYPES, U, dev, f64, rng, wide_rows, within
 from seq_common import lists, on_gpu, packed, places, poison, scan_reference
 
 pytestmark = pytest.mark.gpu
@@ -179,6 +179,38 @@ def test_strided_rows_and_odd_addresses(kind):
     compare(dict(g, y=y), ref, names_of(t), "strided", q)
     for v in [y] + list(out.values()):
         assert (v.as_strided((v.shape[0] - 1, 5), (v.stride(0), 1), v.storage_offset() + v.shape[1]) == 7.0).all()
+
+
+def test_gradients_in_columns_of_one_buffer():
+    """y beside z, dB beside dC and dx beside ddt, as one product reads them."""
+    from paper_2307_07649_amd import tgnn
+    q = packed([40, 2, 90])
+    t, dy = inputs(q, 33, 20, 1, "f32", 12)
+    ref = ref_of(q, t, dy, 1)
+    seqs, (rows, d), n = on_gpu(tgnn, q), t["x"].shape, t["B"].shape[1]
+    zy = torch.full((rows, 2 * d), 7.0, device="cuda")
+    zy[:, :d] = t["z"]
+    y = tgnn.tgnn_selective_scan_fwd(seqs, **{**t, "z": zy[:, :d]}, out=zy[:, d:])
+    bc, xdt = torch.full((rows, 2 * n), 7.0, device="cuda"), torch.full((rows, 2 * d), 7.0, device="cuda")
+    out = dict(dB=bc[:, :n], dC=bc[:, n:], ddt=xdt[:, :d], dx=xdt[:, d:], dz=torch.empty_like(t["z"]))
+    g = tgnn.tgnn_selective_scan_bwd(seqs, dy, **t, out=out)
+    compare(dict(g, y=y), ref, names_of(t), "columns", q)
+    assert (zy[:, :d] == t["z"]).all()
+
+
+def test_more_wavefronts_than_a_grid_has_threads_along_x():
+    """2^32 threads and more: 2^26 + 5 lists of one event, one column, one state (y = C delta x B), over sequences and as single events."""
+    from paper_2307_07649_amd import tgnn
+    n = (1 << 26) + 5
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x, dt, B, C = (torch.rand(n, 1, device="cuda", generator=g) + 0.5 for _ in range(4))
+    A = torch.full((1, 1), -1.0, device="cuda")
+    ref = dt * x * B * C
+    for y in (tgnn.tgnn_selective_scan_fwd(tgnn.Seqs(n, n, 1), x, dt, A, B, C, softplus=False),
+              tgnn.tgnn_selective_scan_step(x, dt, A, B, C, softplus=False)):
+        # three roundings each, and those of three more fused steps that add zero
+        assert ((y - ref).abs() <= 9 * U * ref.abs()).all()
+        del y
 
 
 def test_states_by_index():

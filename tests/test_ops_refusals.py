@@ -205,6 +205,30 @@ def test_scan_outputs_and_workspaces(tgnn):
     assert lib.tgnn_selective_scan_saved_bytes(q, 8, 65) == DIM and lib.tgnn_selective_scan_workspace_bytes(q, 8, 4, 3, 0, 0) == DIM
 
 
+def test_scan_gradients_apart(tgnn):
+    """Gradients of one call share no memory (40 rows of 8 columns)."""
+    lib, q, p = tgnn._lib, make_seqs(tgnn), make_scan(tgnn)
+    at = {k: R + i * 4096 for i, k in enumerate(("dx", "ddt", "dB", "dC", "dz"))}
+    for a, b in (("ddt", "dx"), ("dC", "dB"), ("dz", "ddt")):
+        pitch = {"ld_" + a.lower(): 16, "ld_" + b.lower(): 16}
+        # the same place; its first column is the other's last; its last column is the other's first of the next row
+        for over in ({a: at[b]}, {a: at[b] + 28, **pitch}, {a: at[b] + 36, **pitch}):
+            rc = lib.tgnn_selective_scan_bwd(q, p, P, 8, None, 0, make_grads(tgnn, **{**at, **over}), 0, S, 1 << 20, None)
+            assert rc == INVALID and f"{a} overlaps {b}" in lib.tgnn_last_error().decode(), (a, over)
+
+
+def test_outputs_beside_inputs(tgnn):
+    """An output in other columns of an input's buffer does not overlap it; one column further it does."""
+    lib, q = tgnn._lib, make_seqs(tgnn, n_rows=4000, n_seqs=1, max_len=4000)
+    p = make_scan(tgnn, ld_x=16, dt=Q, B=Q, C=Q, z=Q, A=S, D=S, dt_bias=S, state_in=None)
+    for off in (28, 36, -28, 64 * 7 + 20):
+        assert lib.tgnn_selective_scan_fwd(q, p, P + off, 16, None, None, 0, None, 0, None) == INVALID, off
+        assert "y overlaps" in lib.tgnn_last_error().decode()
+    for off in (32, -32, 64 * 7 + 32):      # (what is refused is the workspace that is not there)
+        assert lib.tgnn_selective_scan_fwd(q, p, P + off, 16, None, None, 0, None, 0, None) == NULL, off
+        assert "workspace" in lib.tgnn_last_error().decode()
+
+
 def test_struct_sizes(tgnn):
     assert C.sizeof(tgnn.tgnn_seqs) == 40 and C.sizeof(tgnn.tgnn_scan) == 24 + 15 * 8 and C.sizeof(tgnn.tgnn_scan_grads) == 13 * 8
 
