@@ -465,7 +465,7 @@ int32_t tgnn_selective_scan_bwd(const tgnn_seqs* seqs, const tgnn_scan* scan, co
 
 /* Layer norm of every row over its n_cols columns: y = (x - mean) rstd weight + bias with rstd = 1 / sqrt(var + eps) and var the
  * mean of (x - mean)^2.  weight, bias [n_cols] or NULL (1, 0); out_mean, out_rstd [n_rows] or NULL: what the backward pass
- * needs.  y may be x itself.  Any n_cols >= 1, n_rows < 2^31 (0: nothing is done). */
+ * needs.  y may be x itself.  1 <= n_cols <= 2^28, n_rows < 2^31 (0: nothing is done). */
 int32_t tgnn_layer_norm_fwd(int32_t dtype, int64_t n_rows, int32_t n_cols, const void* x, int64_t ld_x, const float* weight,
                             const float* bias, float eps, void* y, int64_t ld_y, float* out_mean, float* out_rstd, void* stream);
 /* Its gradients: with xh = (x - mean) rstd and g = dy weight, dx = rstd (g - mean(g) - xh mean(g xh)), d_weight = sum over the rows

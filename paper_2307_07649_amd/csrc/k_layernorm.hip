@@ -303,7 +303,7 @@ static int check_floats(const char* name, const float* p, bool needed) {
 }
 static int check_norm(int32_t dtype, int64_t n_rows, int32_t n_cols) {
   if (!type_known(dtype)) return set_error(TGNN_E_INVALID_ARG, "dtype = %d is none of TGNN_F32, TGNN_BF16, TGNN_F16", dtype);
-  if (n_cols < 1) return set_error(TGNN_E_UNSUPPORTED_DIM, "n_cols = %d", n_cols);
+  if (n_cols < 1 || n_cols > 1 << 28) return set_error(TGNN_E_UNSUPPORTED_DIM, "n_cols = %d outside [1, 2^28]", n_cols);   // (2 n_cols fits an int)
   if (n_rows < 0 || n_rows > INT_MAX) return set_error(TGNN_E_OUT_OF_RANGE, "n_rows = %lld outside [0, 2^31)", (long long)n_rows);
   return TGNN_OK;
 }

@@ -205,6 +205,13 @@ def test_scan_outputs_and_workspaces(tgnn):
     assert lib.tgnn_selective_scan_saved_bytes(q, 8, 65) == DIM and lib.tgnn_selective_scan_workspace_bytes(q, 8, 4, 3, 0, 0) == DIM
 
 
+@pytest.mark.parametrize("cols", [(1 << 28) + 1, (1 << 31) - 1])
+def test_layer_norm_columns(tgnn, cols):
+    for name, (names, args) in (("tgnn_layer_norm_fwd", FWD), ("tgnn_layer_norm_bwd", BWD)):
+        rc, msg = call(tgnn, name, args, names, rows=1, cols=cols)
+        assert rc == DIM and "n_cols" in msg
+
+
 def test_scan_gradients_apart(tgnn):
     """Gradients of one call share no memory (40 rows of 8 columns)."""
     lib, q, p = tgnn._lib, make_seqs(tgnn), make_scan(tgnn)
