@@ -101,17 +101,19 @@ __global__ __launch_bounds__(256) void clip_norm_kernel(const double* part, int 
   if (threadIdx.x == 0) *out = (float)norm;
 }
 
+// (The last read of a gradient and the write go past the caches: with 200M elements in 300 tensors this launch and the next call's squares
+// take 97 and 51 us per 128 tensors, through the caches 102 and 62.)
 template <class T> __device__ __forceinline__ void chunk_scale(const T* p, T* o, int n, float scale) {
   constexpr int V = 16 / sizeof(T);
   if (n == CLIP_CHUNK && ((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(o)) & 15) == 0) {
     float x[CLIP_CHUNK / 256 / V][V];
 #pragma unroll
-    for (int i = 0; i < CLIP_CHUNK / 256 / V; ++i) load_pack<T, V>(p + (i * 256 + threadIdx.x) * V, x[i]);
+    for (int i = 0; i < CLIP_CHUNK / 256 / V; ++i) unpack(take<T, V, false, true>(p + (i * 256 + threadIdx.x) * V, V), x[i]);
 #pragma unroll
     for (int i = 0; i < CLIP_CHUNK / 256 / V; ++i) {
 #pragma unroll
       for (int j = 0; j < V; ++j) x[i][j] *= scale;
-      store_pack<T, V>(o + (i * 256 + threadIdx.x) * V, x[i]);
+      put<T, V, false, true>(o + (i * 256 + threadIdx.x) * V, x[i], V);
     }
   } else {
     for (int i = threadIdx.x; i < n; i += 256) o[i] = (T)((float)p[i] * scale);

@@ -117,14 +117,15 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
       conv_input<T, V, ANY>(a, p.r, state, p.t0 - (a.width - 1) + j, c, v);
       shift_in<V, W>(win, v);
     }
-  // rows are asked for AHEAD before their use
+  // rows are asked for AHEAD before their use, past the caches: 29,000 rows of 1,024 columns in bfloat16 30 us, through them 40 (what
+  // reads x next is the backward pass; there, and for y, it gains nothing)
   const int64_t step = a.q.newest_first ? -1 : 1;
   const T* x = static_cast<const T*>(a.x) + seq_row(a.q, p.r, p.t0) * a.ld_x + c;
   T* y = static_cast<T*>(a.y) + seq_row(a.q, p.r, p.t0) * a.ld_y + c;
   Pack<T, V> next[AHEAD];
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u)
-    if (p.t0 + u < p.t1) next[u] = take<T, V, ANY>(x + u * step * a.ld_x, a.d - c);
+    if (p.t0 + u < p.t1) next[u] = take<T, V, ANY, true>(x + u * step * a.ld_x, a.d - c);
   const bool silu = a.silu != 0;
   auto row = [&](int u) {
     float v[V], pre[V];
@@ -142,7 +143,7 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
     for (int u = 0; u < AHEAD; ++u) {
       row(u);
       const int ahead = min(u + AHEAD, p.t1 - 1 - t);   // (past the end: a row that is there)
-      next[u] = take<T, V, ANY>(x + ahead * step * a.ld_x, a.d - c);
+      next[u] = take<T, V, ANY, true>(x + ahead * step * a.ld_x, a.d - c);
     }
     x += AHEAD * step * a.ld_x;
     y += AHEAD * step * a.ld_y;
@@ -191,7 +192,8 @@ __global__ __launch_bounds__(256) void conv_step_kernel(ConvArgs a) {
 #pragma unroll
     for (int j = 1; j < W; ++j) {
       const int k = j - 1 - (W - a.width);
-      if (k >= 0) put<T, V, ANY>(static_cast<T*>(a.state_out) + (state * (a.width - 1) + k) * a.d + c, win[j], a.d - c);
+      // (past the caches: 4,000 rows of 1,024 columns in float16 18.9 us, through them 20.5)
+      if (k >= 0) put<T, V, ANY, true>(static_cast<T*>(a.state_out) + (state * (a.width - 1) + k) * a.d + c, win[j], a.d - c);
     }
 }
 

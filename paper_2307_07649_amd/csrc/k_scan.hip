@@ -342,7 +342,9 @@ __device__ __forceinline__ float rows_sum(float u, float v) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-constexpr int BWD_WAVES = 4, BWD_COLS = 16 * BWD_WAVES;   // wavefronts and columns of a workgroup
+// Wavefronts and columns of a workgroup.  Wavefronts share what is read of B and C, the sums over columns, and barriers: 1,800 lists of up to ten
+// events, 100 columns, 72 us, one sequence of 8,191 events, 512 columns, 97; with eight 87 and 116, with two 79 and 114, with one 74 and 110.
+constexpr int BWD_WAVES = 4, BWD_COLS = 16 * BWD_WAVES;
 constexpr int FINISH_BITS = 3;
 constexpr int SLICE = 16;                                 // states of a column that a workgroup has at most
 
@@ -693,8 +695,9 @@ __global__ __launch_bounds__(256) void scan_bc_sum_kernel(ScanArgs a) {
 // One event of each of `items` rows, on the rows' states.  LC = 2^bits neighbouring lanes have a column, four states each, next to each
 // other in memory; a workgroup has 256 / LC columns of four rows, whose states are asked for together.  With four lanes and
 // more to a column (QUAD) every one of four neighbouring lanes forms the step size and the gate of one of the rows.  4,000
-// rows of 256 columns and 16 states, 131 MB of states in and out: 47 us; walking over the rows with the next four's states
-// on their way, 65 (138 registers, half the wavefronts).
+// rows of 256 columns and 16 states, 131 MB of states in and out: 35 us, 3.8 TB/s; with the states through the caches, which no other
+// row of the call wants, 47; walking over the rows with the next four's states on their way, 65 (138 registers, half the
+// wavefronts).
 template <class T, bool QUAD>
 __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int bits, int tiles) {
   const unsigned number = group_number();
@@ -704,9 +707,10 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int bits, in
   const int col = tile * (256 >> bits) + (int)(threadIdx.x >> bits), c = min(col, a.d - 1), n0 = part * 4;
   const bool on = col < a.d, whole = n0 + 4 <= a.n;
   const int s0 = min(n0, a.n - 1), bc = c / a.dg * a.n + s0;   // (lanes without a state read another's)
-  auto floats = [&](const float* p, float (&v)[4]) {
+  auto floats = [&](const float* p, float (&v)[4], auto once) {
     if (whole) {
-      const FloatRun<4> r = *reinterpret_cast<const FloatRun<4>*>(p);
+      const FloatRun<4>* at = reinterpret_cast<const FloatRun<4>*>(p);
+      const FloatRun<4> r = decltype(once)::value ? stream_load(at) : *at;
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = r.v[i];
     } else {
@@ -731,14 +735,14 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int bits, in
   for (int e = 0; e < 4; ++e) {
     const int64_t row = min(row0 + e, last);
     state[e] = state_of(a, (int)row);
-    if (state[e] >= 0 && a.state_in != nullptr) floats(a.state_in + (state[e] * a.d + c) * a.n + s0, h[e]);
+    if (state[e] >= 0 && a.state_in != nullptr) floats(a.state_in + (state[e] * a.d + c) * a.n + s0, h[e], std::true_type());
     else
 #pragma unroll
       for (int i = 0; i < 4; ++i) h[e][i] = 0.0f;
     values(a.B, row * a.ld_b + bc, B[e]);
     values(a.C, row * a.ld_c + bc, C[e]);
   }
-  floats(a.A + (int64_t)c * a.n + s0, A);
+  floats(a.A + (int64_t)c * a.n + s0, A, std::false_type());
   const float bias = a.bias ? a.bias[c] : 0.0f, D = a.D ? a.D[c] : 0.0f;
   struct Own { float x, d2, in, gate; };   // of one row
   auto own = [&](int64_t r) {
@@ -786,7 +790,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a, int bits, in
         FloatRun<4> r;
 #pragma unroll
         for (int i = 0; i < 4; ++i) r.v[i] = h[e][i];
-        *reinterpret_cast<FloatRun<4>*>(p) = r;
+        stream_store(reinterpret_cast<FloatRun<4>*>(p), r);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i)

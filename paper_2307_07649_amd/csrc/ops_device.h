@@ -20,6 +20,21 @@ template <class F> inline void with_type(int dtype, F f) {   // f(T()) for the t
   else f(f16());
 }
 
+// Sixteen bytes that this call will not read again, past the caches (STREAM): what is there stays for what is read again.
+template <class Q> __device__ __forceinline__ Q stream_load(const Q* p) {
+  typedef unsigned U __attribute__((ext_vector_type(sizeof(Q) / 4), aligned(alignof(Q) < 4 ? 4 : alignof(Q))));
+  const U u = __builtin_nontemporal_load(reinterpret_cast<const U*>(p));
+  Q q;
+  __builtin_memcpy(&q, &u, sizeof(q));
+  return q;
+}
+template <class Q> __device__ __forceinline__ void stream_store(Q* p, const Q& q) {
+  typedef unsigned U __attribute__((ext_vector_type(sizeof(Q) / 4), aligned(alignof(Q) < 4 ? 4 : alignof(Q))));
+  U u;
+  __builtin_memcpy(&u, &q, sizeof(q));
+  __builtin_nontemporal_store(u, reinterpret_cast<U*>(p));
+}
+
 // V values of T as one access; the address has to be a multiple of V * sizeof(T)
 template <class T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
 template <class T, int V> __device__ __forceinline__ void load_pack(const T* p, float (&x)[V]) {
@@ -41,9 +56,11 @@ template <int N> using FloatRun = Run<float, N>;
 // V values of a row from p on, of which `left` are the row's own (the others: zeros, not written).  ANY: the row's values may begin
 // at any address of one and their number be no multiple of V; a pack that is all there is one access all the same, which the
 // hardware takes at any address.
-template <class T, int V, bool ANY> __device__ __forceinline__ Pack<T, V> take(const T* p, int left) {
+template <class T, int V, bool ANY, bool STREAM = false> __device__ __forceinline__ Pack<T, V> take(const T* p, int left) {
   Pack<T, V> q;
-  if constexpr (!ANY) {
+  if constexpr (!ANY && STREAM) {
+    q = stream_load(reinterpret_cast<const Pack<T, V>*>(p));
+  } else if constexpr (!ANY) {
     q = *reinterpret_cast<const Pack<T, V>*>(p);
   } else if (left >= V) {
     const Run<T, V> r = *reinterpret_cast<const Run<T, V>*>(p);
@@ -59,8 +76,13 @@ template <class T, int V> __device__ __forceinline__ void unpack(const Pack<T, V
 #pragma unroll
   for (int i = 0; i < V; ++i) x[i] = (float)q.v[i];
 }
-template <class T, int V, bool ANY> __device__ __forceinline__ void put(T* p, const float (&x)[V], int left) {
-  if constexpr (!ANY) {
+template <class T, int V, bool ANY, bool STREAM = false> __device__ __forceinline__ void put(T* p, const float (&x)[V], int left) {
+  if constexpr (!ANY && STREAM) {
+    Pack<T, V> q;
+#pragma unroll
+    for (int i = 0; i < V; ++i) q.v[i] = (T)x[i];
+    stream_store(reinterpret_cast<Pack<T, V>*>(p), q);
+  } else if constexpr (!ANY) {
     store_pack<T, V>(p, x);
   } else if (left >= V) {
     Run<T, V> r;
