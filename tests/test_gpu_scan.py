@@ -370,3 +370,40 @@ def test_same_result_every_time_streams_and_graphs():
         assert all(torch.equal(a, b) for a, b in zip(out, first))
         assert all(torch.equal(a, b) for a, b in zip(both(), first))
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("n,saved", [(16, False), (40, True), (64, False)])
+def test_two_captured_calls_of_their_own_workspaces(n, saved):
+    """Two graphs of different calls, replayed in turn and on two streams at once: neither finds the other's scratch memory."""
+    from paper_2307_07649_amd import tgnn
+    calls = []
+    for seed, q in ((1, packed([210, 0, 33])), (2, packed([9, 120, 77, 1]))):
+        t, dy = inputs(q, 70, n, 1, "f32", seed)
+        calls.append((on_gpu(tgnn, q), t, dy))
+
+    def run_one(seqs, t, dy):
+        sv = tgnn.selective_scan_saved(seqs, t["A"]) if saved else None
+        y = tgnn.tgnn_selective_scan_fwd(seqs, **t, saved=sv)
+        g = tgnn.tgnn_selective_scan_bwd(seqs, dy, **t, saved=sv)
+        return [y] + [g[k] for k in sorted(g)]
+    first = [[v.clone() for v in run_one(*c)] for c in calls]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for c in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(run_one(*c))
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(3):
+        for o in outs:
+            for v in o:
+                v.fill_(3)
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for o, f in zip(outs, first):
+            assert all(torch.equal(a, b) for a, b in zip(o, f))
+        again = run_one(*calls[0])
+        assert all(torch.equal(a, b) for a, b in zip(again, first[0]))
