@@ -463,12 +463,13 @@ def _tensor_list(tensors, name, like=None):
     if not ts:
         return array("Q"), array("q"), array("i"), None
     # (one pass of a built-in per property: several hundred tensors a call)
-    if not all(map(torch.Tensor.is_contiguous, ts)) or not {t.dtype for t in ts} <= _DTYPES.keys():
+    kind = array("i", [_DTYPES.get(t.dtype, -1) for t in ts])
+    if not all(map(torch.Tensor.is_contiguous, ts)) or -1 in kind:
         raise ValueError(f"{name}: contiguous tensors of float32, bfloat16 or float16 are needed")
     dev = _device_of(ts[0])
     if set(map(torch.Tensor.get_device, ts)) != {dev}:
         raise ValueError(f"{name}: tensors on the current GPU are needed")
-    numel, kind = array("q", map(torch.Tensor.numel, ts)), array("i", [_DTYPES[t.dtype] for t in ts])
+    numel = array("q", map(torch.Tensor.numel, ts))
     if like is not None and (numel != like[1] or kind != like[2]):
         raise ValueError(f"{name}: tensors of the gradients' sizes and types are needed")
     return array("Q", map(torch.Tensor.data_ptr, ts)), numel, kind, ts[0].device
