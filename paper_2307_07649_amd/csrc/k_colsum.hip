@@ -9,7 +9,7 @@ namespace tgnn {
 __global__ __launch_bounds__(1024) void column_sum_kernel(ColumnSum a) {
   __shared__ double parts[16][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t m = (int64_t)blockIdx.x * 16 + (threadIdx.x & 15);
+  const int64_t m = (int64_t)group_number() * 16 + (threadIdx.x & 15);
   double sum = 0.0;
   if (m < a.cols) {
 #pragma unroll 4
@@ -33,7 +33,7 @@ __global__ __launch_bounds__(1024) void column_sum_kernel(ColumnSum a) {
 
 void column_sum(const ColumnSum& a, hipStream_t s) {
   if (a.cols <= 0) return;
-  hipLaunchKernelGGL(column_sum_kernel, dim3((unsigned)((a.cols + 15) / 16)), dim3(1024), 0, s, a);
+  hipLaunchKernelGGL(column_sum_kernel, group_grid((a.cols + 15) / 16, 1024), dim3(1024), 0, s, a);
 }
 
 }  // namespace tgnn

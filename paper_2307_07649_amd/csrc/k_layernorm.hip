@@ -110,7 +110,8 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_fwd_kernel(NormArgs a) {
 template <class T>
 __global__ __launch_bounds__(256) void norm_fwd_wide_kernel(NormArgs a) {
   __shared__ float parts[4];
-  const int64_t row = blockIdx.x;
+  const int64_t row = group_number();
+  if (row >= a.rows) return;
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
   float sum = 0.0f;
   for (int c = threadIdx.x; c < a.cols; c += 256) sum += (float)x[c];
@@ -225,7 +226,8 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(NormArgs a) {
 template <class T>
 __global__ __launch_bounds__(256) void norm_bwd_wide_kernel(NormArgs a) {
   __shared__ float parts[4];
-  const int64_t row = blockIdx.x;
+  const int64_t row = group_number();
+  if (row >= a.rows) return;
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
   const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
   const float mean = a.mean[row], rstd = a.rstd[row];
@@ -346,7 +348,7 @@ extern "C" int32_t tgnn_layer_norm_fwd(int32_t dtype, int64_t n_rows, int32_t n_
       if (fit) hipLaunchKernelGGL((norm_fwd_kernel<T, V, G, K, false>), grid, dim3(THREADS), 0, s, a);
       else hipLaunchKernelGGL((norm_fwd_kernel<T, V, G, K, true>), grid, dim3(THREADS), 0, s, a);
     });
-    if (!fits) hipLaunchKernelGGL((norm_fwd_wide_kernel<T>), dim3((unsigned)n_rows), dim3(256), 0, s, a);
+    if (!fits) hipLaunchKernelGGL((norm_fwd_wide_kernel<T>), group_grid(n_rows), dim3(256), 0, s, a);
   });
   TGNN_LAUNCH_CHECK();
   return TGNN_OK;
@@ -405,7 +407,7 @@ extern "C" int32_t tgnn_layer_norm_bwd(int32_t dtype, int64_t n_rows, int32_t n_
         n_part = (int)(n_rows < NORM_WIDE_PARTS ? n_rows : NORM_WIDE_PARTS);
         hipLaunchKernelGGL((norm_bwd_wide_weights_kernel<T>), dim3((n_cols + 255) / 256, n_part), dim3(256), 0, s, a);
       }
-      hipLaunchKernelGGL((norm_bwd_wide_kernel<T>), dim3((unsigned)n_rows), dim3(256), 0, s, a);
+      hipLaunchKernelGGL((norm_bwd_wide_kernel<T>), group_grid(n_rows), dim3(256), 0, s, a);
     });
     TGNN_LAUNCH_CHECK();
   }

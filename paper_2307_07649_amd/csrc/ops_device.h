@@ -133,11 +133,11 @@ inline bool rows_overlap(int64_t rows, int size, const RowArray& a, const RowArr
   return from < (uintptr_t)a.cols * size || from + (uintptr_t)b.cols * size > pitch;
 }
 
-// A launch of n workgroups of 256 threads, n <= INT_MAX: a grid has fewer than 2^32 threads along x, so that the workgroups of a larger one
-// are spread over y as well.  Some may lie behind the last one: a kernel has to look at its number.
-inline dim3 group_grid(int64_t n) {
-  constexpr int64_t ROW = 1 << 23;
-  return n <= ROW ? dim3((unsigned)n) : dim3((unsigned)ROW, (unsigned)((n + ROW - 1) / ROW));
+// A launch of n <= INT_MAX workgroups of at most `threads` threads: a grid has fewer than 2^32 threads along x, so that the workgroups of a
+// larger one are spread over y as well.  Some may lie behind the last one: a kernel has to look at its number.
+inline dim3 group_grid(int64_t n, int threads = 256) {
+  const int64_t row = (int64_t(1) << 31) / threads;
+  return n <= row ? dim3((unsigned)n) : dim3((unsigned)row, (unsigned)((n + row - 1) / row));
 }
 __device__ __forceinline__ unsigned group_number() { return blockIdx.y * gridDim.x + blockIdx.x; }
 
