@@ -21,14 +21,14 @@ namespace tgnn {
 constexpr int norm_threads(int g) { return g > 256 ? g : 256; }   // of a workgroup
 
 // sum over the G neighbouring threads that have a row
-template <int G> __device__ __forceinline__ float row_sum(float v, float* parts) {
+template <int G, class S> __device__ __forceinline__ S row_sum(S v, S* parts) {
 #pragma unroll
   for (int o = (G < 64 ? G : 64) / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
   if constexpr (G > 64) {
     __syncthreads();   // the parts of the sum before this one have been read
     if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = 0.0f;
+    v = 0;
 #pragma unroll
     for (int w = 0; w < G / 64; ++w) v += parts[w];
   }
@@ -105,20 +105,24 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_fwd_kernel(NormArgs a) {
   }
 }
 
-// Rows wider than the registers: three passes, the second and third out of the L2 (8,191 rows of 4,096 in bfloat16 taken this way 87
-// us, and 124 backward).
+// Rows wider than the registers: three passes, the second and third out of the L2.  A thread has a 256th of a row: its sums are held in
+// double, so that errors do not grow with the columns (2,048 rows of 16,384 in bfloat16: 67 us, 2.0 TB/s, and 94 backward; with float
+// sums 64 and 92).
 template <class T>
 __global__ __launch_bounds__(256) void norm_fwd_wide_kernel(NormArgs a) {
-  __shared__ float parts[4];
+  __shared__ double parts[4];
   const int64_t row = group_number();
   if (row >= a.rows) return;
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
-  float sum = 0.0f;
-  for (int c = threadIdx.x; c < a.cols; c += 256) sum += (float)x[c];
-  const float mean = row_sum<256>(sum, parts) / (float)a.cols;
-  sum = 0.0f;
-  for (int c = threadIdx.x; c < a.cols; c += 256) sum += ((float)x[c] - mean) * ((float)x[c] - mean);
-  const float rstd = 1.0f / sqrtf(row_sum<256>(sum, parts) / (float)a.cols + a.eps);
+  double sum = 0.0;
+  for (int c = threadIdx.x; c < a.cols; c += 256) sum += (double)(float)x[c];
+  const double exact = row_sum<256>(sum, parts) / a.cols;
+  sum = 0.0;
+  for (int c = threadIdx.x; c < a.cols; c += 256) {
+    const double d = (double)(float)x[c] - exact;
+    sum = fma(d, d, sum);
+  }
+  const float mean = (float)exact, rstd = (float)(1.0 / sqrt(row_sum<256>(sum, parts) / a.cols + (double)a.eps));
   if (threadIdx.x == 0) {
     if (a.out_mean) a.out_mean[row] = mean;
     if (a.out_rstd) a.out_rstd[row] = rstd;
@@ -225,20 +229,19 @@ __global__ __launch_bounds__(norm_threads(G)) void norm_bwd_kernel(NormArgs a) {
 // Rows wider than the registers: the rows' gradients (x and dy twice, the second time out of the L2), after ...
 template <class T>
 __global__ __launch_bounds__(256) void norm_bwd_wide_kernel(NormArgs a) {
-  __shared__ float parts[4];
+  __shared__ double parts[4];
   const int64_t row = group_number();
   if (row >= a.rows) return;
   const T* x = static_cast<const T*>(a.x) + row * a.ld_x;
   const T* dy = static_cast<const T*>(a.dy) + row * a.ld_dy;
   const float mean = a.mean[row], rstd = a.rstd[row];
-  float s1 = 0.0f, s2 = 0.0f;
+  double sum1 = 0.0, sum2 = 0.0;
   for (int c = threadIdx.x; c < a.cols; c += 256) {
     const float g = (float)dy[c] * (a.weight ? a.weight[c] : 1.0f);
-    s1 += g;
-    s2 += g * (((float)x[c] - mean) * rstd);
+    sum1 += (double)g;
+    sum2 += (double)(g * (((float)x[c] - mean) * rstd));
   }
-  s1 = row_sum<256>(s1, parts) / (float)a.cols;
-  s2 = row_sum<256>(s2, parts) / (float)a.cols;
+  const float s1 = (float)(row_sum<256>(sum1, parts) / a.cols), s2 = (float)(row_sum<256>(sum2, parts) / a.cols);
   T* dx = static_cast<T*>(a.y) + row * a.ld_y;
   for (int c = threadIdx.x; c < a.cols; c += 256) {
     const float g = (float)dy[c] * (a.weight ? a.weight[c] : 1.0f);
@@ -250,15 +253,15 @@ template <class T>
 __global__ __launch_bounds__(256) void norm_bwd_wide_weights_kernel(NormArgs a) {
   const int c = blockIdx.x * 256 + threadIdx.x;
   if (c >= a.cols) return;
-  float dw = 0.0f, db = 0.0f;
+  double dw = 0.0, db = 0.0;
   for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
     const float d = (float)static_cast<const T*>(a.dy)[row * a.ld_dy + c];
-    dw += d * (((float)static_cast<const T*>(a.x)[row * a.ld_x + c] - a.mean[row]) * a.rstd[row]);
-    db += d;
+    dw += (double)(d * (((float)static_cast<const T*>(a.x)[row * a.ld_x + c] - a.mean[row]) * a.rstd[row]));
+    db += (double)d;
   }
   float* part = a.part + (int64_t)blockIdx.y * 2 * a.cols;
-  part[c] = dw;
-  part[a.cols + c] = db;
+  part[c] = (float)dw;
+  part[a.cols + c] = (float)db;
 }
 
 constexpr int NORM_FWD_GRID = 2048;   // workgroups of the forward pass: eight to a compute unit
