@@ -539,6 +539,15 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_bwd_kernel(ScanArgs a)
             y[e] = fmaf(h[i], sC[(4 * j + e) * N4 + q * NP + i], y[e]);
           }
         }
+        auto columns_only = [&]() {   // a column that is none adds nothing, also where B (its state is not zero then) or C is infinite
+          if (full) return;
+          asm volatile("");   // (a branch, not 16 selects for every wavefront)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int i = 0; i < NP; ++i) v4[e][i] = on ? v4[e][i] : 0.0f;
+        };
+        columns_only();
         column_sums<NP>(v4, sum);
         const int at = (4 * j + event_of_sum(lane)) * N4 + q * NP;
         if ((lane & 12) == 0)
@@ -557,13 +566,7 @@ __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_bwd_kernel(ScanArgs a)
             g[i] = dec[e][i] * lam;
           }
         }
-        if (!full) {   // a column that is none adds nothing, also where C is infinite
-          asm volatile("");   // (a branch, not 16 selects for every wavefront)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-#pragma unroll
-            for (int i = 0; i < NP; ++i) v4[e][i] = on ? v4[e][i] : 0.0f;
-        }
+        columns_only();
         column_sums<NP>(v4, sum);
         if ((lane & 12) == 0)
 #pragma unroll
