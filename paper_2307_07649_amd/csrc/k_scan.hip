@@ -257,6 +257,14 @@ __global__ __launch_bounds__(256) void scan_fwd_kernel(ScanArgs a) {
   }
 }
 
+// v 2^s for the deltas of a whole segment or run: the factor may be more (or less) than a float holds where no event's is, and where the
+// product is not (zero, a state that grows from 1e-30 to 1e11); outside [-400, 400] the product is zero or infinite whatever v is.
+__device__ __forceinline__ float times_exp2(float v, float s) {
+  s = fminf(fmaxf(s, -400.0f), 400.0f);
+  const float whole = floorf(s);
+  return ldexpf(v * __builtin_amdgcn_exp2f(s - whole), (int)whole);
+}
+
 // From segment to segment.  Forward: seg_state[k] becomes the state before segment k, from the sequence's first state; backward: what
 // reaches segment k from behind, from zero.  A thread has a column and state of a sequence and asks for eight segments at a time;
 // where there are many of them (RUNS = 8) eight threads cut them into runs: each run's own part and the sum of its
@@ -294,7 +302,7 @@ __global__ __launch_bounds__(256) void scan_chain_kernel(ScanArgs a) {
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      cur = fmaf(__builtin_amdgcn_exp2f(d[u] * A), cur, v[u]);
+      cur = times_exp2(cur, d[u] * A) + v[u];
       total += d[u];
     }
   }
@@ -305,7 +313,7 @@ __global__ __launch_bounds__(256) void scan_chain_kernel(ScanArgs a) {
   }
   if (!on) return;
   cur = !BACK && state >= 0 && a.state_in != nullptr ? a.state_in[state * dn + e] : 0.0f;
-  for (int i = 0; i < run; ++i) cur = fmaf(__builtin_amdgcn_exp2f(sum[i][x] * A), cur, part[i][x]);
+  for (int i = 0; i < run; ++i) cur = times_exp2(cur, sum[i][x] * A) + part[i][x];
   for (int k = k0; k < k1; k += U) {
     float v[U], d[U];
 #pragma unroll
@@ -318,7 +326,7 @@ __global__ __launch_bounds__(256) void scan_chain_kernel(ScanArgs a) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (k + u < k1) a.seg_state[at(k + u) * dn + e] = cur;
-      cur = fmaf(__builtin_amdgcn_exp2f(d[u] * A), cur, v[u]);
+      cur = times_exp2(cur, d[u] * A) + v[u];
     }
   }
 }

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from ops_common import dev, rng
+from ops_common import U, dev, f64, rng, within
 from seq_common import on_gpu, packed
 
 pytestmark = pytest.mark.gpu
@@ -24,3 +24,44 @@ def test_an_infinite_B_makes_dC_infinite(d, n):
     assert (got[2:, n - 1] == float("inf")).all()
     got[2:, n - 1] = clean[2:, n - 1]
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("rows", [200, 3000])      # segments walked by one thread, and in runs
+def test_a_segment_may_multiply_by_more_than_a_float_holds(rows):
+    """A delta = 3 in every event: 2^138 over 32 of them.  A state that is zero stays zero through such segments: inputs in the last twenty
+    events only, gradients of the first twenty only, in segments and in one walk alike."""
+    from paper_2307_07649_amd import tgnn
+    q, g, d, n = packed([rows]), rng(rows), 3, 2
+    t = dict(x=dev(g.standard_normal((rows, d)), torch.float32), dt=torch.full((rows, d), 3.0, device="cuda"),
+             B=dev(g.standard_normal((rows, n)), torch.float32), C=dev(g.standard_normal((rows, n)), torch.float32),
+             A=torch.ones(d, n, device="cuda"))
+    dy = dev(g.standard_normal((rows, d)), torch.float32)
+    t["x"][:-20] = 0
+    dy[20:] = 0
+    runs = {}
+    for whole in (False, True):
+        seqs = on_gpu(tgnn, q, max_len=8) if whole else on_gpu(tgnn, q)
+        assert (tgnn._lib.tgnn_selective_scan_workspace_bytes(seqs.c, d, n, 1, 0, 0) == 0) == whole
+        y = tgnn.tgnn_selective_scan_fwd(seqs, **t, softplus=False)
+        runs[whole] = [y] + list(tgnn.tgnn_selective_scan_bwd(seqs, dy, **t, softplus=False).values())
+        assert torch.isfinite(y).all() and (y[-1] != 0).all() and (y[:-20] == 0).all()
+        assert torch.isfinite(runs[whole][1]).all() and (runs[whole][1][0] != 0).all()
+    assert all(torch.equal(a, b) for a, b in zip(*runs.values()))
+
+
+@pytest.mark.parametrize("rows", [200, 3000])
+@pytest.mark.parametrize("start,step", [(1e-30, 3.0), (1e30, -3.0)])
+def test_a_state_that_changes_by_more_than_a_float_holds(rows, start, step):
+    """The first 32 events multiply a stored state by exp(+-96), the others keep it.  The factor is an exponential of a sum of 32 terms, in
+    base 2: off by at most (32 + 2) U times the exponent, and a few roundings."""
+    from paper_2307_07649_amd import tgnn
+    q, d, n = packed([rows]), 2, 3
+    dt = torch.zeros(rows, d, device="cuda")
+    dt[:32] = abs(step)
+    zero, one = torch.zeros(rows, d, device="cuda"), torch.ones(rows, n, device="cuda")
+    state, end = torch.full((1, d, n), start, device="cuda"), torch.zeros(1, d, n, device="cuda")
+    A = torch.full((d, n), step / abs(step), device="cuda")
+    y = tgnn.tgnn_selective_scan_fwd(on_gpu(tgnn, q), zero, dt, A, one, one, softplus=False, state_in=state, state_out=end)
+    want = f64(state) * torch.exp(torch.tensor(32.0 * step, dtype=torch.float64))
+    within(end, want, (34 * 96 * U + 8 * U) * want, "state")
+    within(y[32:].cpu(), (n * want[0, 0, 0]).expand(rows - 32, d), (34 * 96 * U + 16 * U) * n * want[0, 0, 0], "y")
