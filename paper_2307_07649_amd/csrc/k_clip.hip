@@ -104,7 +104,7 @@ __global__ __launch_bounds__(256) void clip_norm_kernel(const double* part, int 
 
 // (The last read of a gradient and the write go past the caches: with 200M elements in 300 tensors this launch and the next call's squares
 // take 97 and 51 us per 128 tensors, through the caches 102 and 62.)
-template <class T> __device__ __forceinline__ void chunk_scale(const T* p, T* o, int n, float scale) {
+template <class T> __device__ __forceinline__ void chunk_scale(const T* p, T* o, int n, double scale) {
   constexpr int V = 16 / sizeof(T);
   if (n == CLIP_CHUNK && ((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(o)) & 15) == 0) {
     float x[CLIP_CHUNK / 256 / V][V];
@@ -113,25 +113,26 @@ template <class T> __device__ __forceinline__ void chunk_scale(const T* p, T* o,
 #pragma unroll
     for (int i = 0; i < CLIP_CHUNK / 256 / V; ++i) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) x[i][j] *= scale;
+      for (int j = 0; j < V; ++j) x[i][j] = (float)((double)x[i][j] * scale);
       put<T, V, false, true>(o + (i * 256 + threadIdx.x) * V, x[i], V);
     }
   } else {
-    for (int i = threadIdx.x; i < n; i += 256) o[i] = (T)((float)p[i] * scale);
+    for (int i = threadIdx.x; i < n; i += 256) o[i] = (T)(float)((double)(float)p[i] * scale);
   }
 }
 
-// A norm that is no finite number scales nothing: the gradients stay (or are copied) as they are, and the norm says so.
-__device__ __forceinline__ float clip_scale(double norm, float max_norm) {
-  return norm > (double)max_norm && norm < HUGE_VAL ? (float)((double)max_norm / norm) : 1.0f;
+// A norm that is no finite number scales nothing: the gradients stay (or are copied) as they are, and the norm says so.  The factor is
+// held in double, and so are its products: with gradients of 1e38 it is smaller than a float holds, and they are not.
+__device__ __forceinline__ double clip_scale(double norm, float max_norm) {
+  return norm > (double)max_norm && norm < HUGE_VAL ? (double)max_norm / norm : 1.0;
 }
 
 __global__ __launch_bounds__(256) void clip_scale_kernel(ClipArgs a) {
   const double norm = norm_of_parts(a.part, a.n_part);
   if (a.write_norm && blockIdx.x == 0 && threadIdx.x == 0) *a.out_norm = (float)norm;
-  const float scale = clip_scale(norm, a.max_norm);
+  const double scale = clip_scale(norm, a.max_norm);
   clip_chunks(a, [&](int t, int type, int64_t at, int n) {
-    if (scale == 1.0f && a.dst[t] == a.src[t]) return;
+    if (scale == 1.0 && a.dst[t] == a.src[t]) return;
     if (type == TGNN_F32) chunk_scale(static_cast<const float*>(a.src[t]) + at, static_cast<float*>(a.dst[t]) + at, n, scale);
     else if (type == TGNN_BF16) chunk_scale(static_cast<const bf16*>(a.src[t]) + at, static_cast<bf16*>(a.dst[t]) + at, n, scale);
     else chunk_scale(static_cast<const f16*>(a.src[t]) + at, static_cast<f16*>(a.dst[t]) + at, n, scale);

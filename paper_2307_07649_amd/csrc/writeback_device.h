@@ -86,7 +86,7 @@ __device__ __forceinline__ void rank_sum_block(const RankSum& a, int block) {
 }
 
 // The optimiser's update: 64 blocks per tensor, block x of tensor t.  `scale`: of the gradients (1 unless they are clipped).
-__device__ __forceinline__ void param_update_block(const SgdSet& set, const AdamSet* adam, int t, int x, float lr, float scale) {
+__device__ __forceinline__ void param_update_block(const SgdSet& set, const AdamSet* adam, int t, int x, float lr, double scale) {
   float* p = set.p[t];
   const float* g = set.g[t];
   const int n = set.n[t];
@@ -98,7 +98,7 @@ __device__ __forceinline__ void param_update_block(const SgdSet& set, const Adam
     const float c1 = (float)(1.0 / (1.0 - pow((double)ad.beta1, steps)));
     const float c2 = (float)(1.0 / (1.0 - pow((double)ad.beta2, steps)));
     for (int i = x * 256 + threadIdx.x; i < n; i += 64 * 256) {
-      const float gi = g[i] * scale;
+      const float gi = (float)((double)g[i] * scale);
       const float mi = ad.beta1 * m[i] + (1.0f - ad.beta1) * gi;
       const float vi = ad.beta2 * v[i] + (1.0f - ad.beta2) * gi * gi;
       m[i] = mi;
@@ -107,7 +107,7 @@ __device__ __forceinline__ void param_update_block(const SgdSet& set, const Adam
     }
     return;
   }
-  for (int i = x * 256 + threadIdx.x; i < n; i += 64 * 256) p[i] -= lr * (g[i] * scale);
+  for (int i = x * 256 + threadIdx.x; i < n; i += 64 * 256) p[i] -= lr * (float)((double)g[i] * scale);
 }
 
 // block: 0 .. wb_total_blocks(a) - 1
@@ -120,7 +120,7 @@ __device__ __forceinline__ void wb_sgd_block(const WbArgs& a, int block) {
       else if (a.rr.rank != nullptr) rank_sum_block(a.rr, extra - n_sgd - a.stat.blocks);
       return;
     }
-    param_update_block(*a.sgd, a.adam, extra >> 6, extra & 63, a.lr, 1.0f);
+    param_update_block(*a.sgd, a.adam, extra >> 6, extra & 63, a.lr, 1.0);
     return;
   }
   if (a.vec == 4) wb_scatter_block<4>(a, block);
