@@ -198,6 +198,13 @@ def _elsewhere(t, name):
     return ValueError(f"{name} is on {t.device}: a tensor on the current GPU is needed")
 
 
+def _int32(n, name):
+    """n, which the library takes as an int32 (ctypes would hand on its low 32 bits alone)."""
+    if not -0x80000000 <= n <= 0x7fffffff:
+        raise ValueError(f"{name} = {n} is outside what 32 bits hold")
+    return n
+
+
 def _rows(t, name, dev, dtype=None, shape=None):
     """(pointer, row distance) of a row array: two dimensions, values of a row next to each other; dtype, shape: what it has to be."""
     s = t.shape
@@ -209,6 +216,8 @@ def _rows(t, name, dev, dtype=None, shape=None):
     n, c = s
     if one != 1 and c > 1 and n > 0:
         raise ValueError(f"{name}: the values of a row have to be contiguous")
+    if c > 0x7fffffff:
+        raise ValueError(f"{name}: {c} columns are more than 32 bits hold")
     if t.get_device() != dev:
         raise _elsewhere(t, name)
     return t.data_ptr(), (ld if n > 1 else c)
@@ -252,8 +261,8 @@ class Seqs:
                 if t.get_device() != _device_of(t):
                     raise _elsewhere(t, name)
         self.indptr, self.cnt, self.n_rows, self.n_seqs = indptr, cnt, n_rows, n_seqs
-        self.c = tgnn_seqs(None if indptr is None else indptr.data_ptr(), None if cnt is None else cnt.data_ptr(), n_rows, n_seqs,
-                           max_len, 1 if newest_first else 0)
+        self.c = tgnn_seqs(None if indptr is None else indptr.data_ptr(), None if cnt is None else cnt.data_ptr(), n_rows,
+                           _int32(n_seqs, "n_seqs"), _int32(max_len, "max_len"), 1 if newest_first else 0)
 
 
 def _seq_rows(seqs, x):
@@ -271,7 +280,7 @@ def _states(state_in, state_out, state_idx, dev, n, shape, dtype):
                 raise ValueError(f"{name}: a contiguous {dtype} tensor {('n_states',) + shape} is needed, not {tuple(s)} {t.dtype}")
             if t.get_device() != dev:
                 raise _elsewhere(t, name)
-            states = s[0]
+            states = _int32(s[0], "n_states")
         ptr.append(None if t is None else t.data_ptr())
     if state_idx is not None:
         if state_idx.dtype != torch.int32 or state_idx.shape != (n,) or not state_idx.is_contiguous():
@@ -292,7 +301,7 @@ def tgnn_causal_conv_fwd(seqs, x, weight, bias=None, silu=True, state_in=None, s
     _seq_rows(seqs, x)
     dev = _device_of(x)
     px, ldx = _rows(x, "x", dev)
-    d, w = x.shape[1], weight.shape[-1]
+    d, w = x.shape[1], _int32(weight.shape[-1], "width")
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
     py, ldy = _rows(y, "out", dev, x.dtype, x.shape)
     si, so, ix, ns = _states(state_in, state_out, state_idx, dev, seqs.n_seqs, (w - 1, d), x.dtype)
@@ -306,7 +315,7 @@ def tgnn_causal_conv_step(x, weight, bias=None, silu=True, state_in=None, state_
     dev = _device_of(x)
     px, ldx = _rows(x, "x", dev)
     n, d = x.shape
-    w = weight.shape[-1]
+    w = _int32(weight.shape[-1], "width")
     y = torch.empty(n, d, dtype=x.dtype, device=x.device) if out is None else out
     py, ldy = _rows(y, "out", dev, x.dtype, x.shape)
     si, so, ix, ns = _states(state_in, state_out, state_idx, dev, n, (w - 1, d), x.dtype)
@@ -322,7 +331,7 @@ def tgnn_causal_conv_bwd(seqs, dy, x, weight, bias=None, silu=True, state_in=Non
     dev = _device_of(x)
     px, ldx = _rows(x, "x", dev)
     pdy, lddy = _rows(dy, "dy", dev, x.dtype, x.shape)
-    d, w = x.shape[1], weight.shape[-1]
+    d, w = x.shape[1], _int32(weight.shape[-1], "width")
     dx = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
     pdx, lddx = _rows(dx, "out", dev, x.dtype, x.shape)
     (dw, db), add = _weight_grads((d_weight, d_bias), ((d, w), (d,)), x.device)
@@ -360,7 +369,9 @@ def _bytes(n):
 
 def selective_scan_saved(seqs, A):
     """A buffer that tgnn_selective_scan_fwd fills for tgnn_selective_scan_bwd (the states every 32 events)."""
-    return torch.empty(_bytes(_lib.tgnn_selective_scan_saved_bytes(seqs.c, *A.shape)) // 4, dtype=torch.float32, device=A.device)
+    d, n = A.shape
+    need = _bytes(_lib.tgnn_selective_scan_saved_bytes(seqs.c, _int32(d, "d"), _int32(n, "n_state")))
+    return torch.empty(need // 4, dtype=torch.float32, device=A.device)
 
 
 def _saved(saved, dev):
