@@ -714,8 +714,9 @@ class Context:
 
     def tgnn_set_grad_clip(self, max_norm, out_norm=None):
         """max_norm of the in-step update's gradients, 0: none; out_norm: float32 device tensor [1], every step's norm."""
+        norm = None if out_norm is None else _floats(out_norm, "out_norm", _device_of(out_norm), (1,))
+        _check(_lib.tgnn_set_grad_clip(self.h, max_norm, norm))
         self._clip_norm = out_norm      # keeps it alive
-        _check(_lib.tgnn_set_grad_clip(self.h, max_norm, _ptr(out_norm)))
 
     def tgnn_train_static(self, enable, grad_static=None, lr_static=0.0):
         self._gstat = grad_static

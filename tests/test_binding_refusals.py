@@ -45,3 +45,15 @@ def test_states_that_32_bits_do_not_count(tgnn):
         st = types.SimpleNamespace(shape=(BIG, 8, 4), dtype=torch.float32, is_contiguous=lambda: True, get_device=lambda: None, data_ptr=lambda: 0)
         with pytest.raises(ValueError, match="n_states"):
             tgnn.tgnn_selective_scan_fwd(q, x, x, meta(8, 4), meta(1, 4), meta(1, 4), state_idx=idx, **{k: st})
+
+
+def test_where_the_steps_norm_goes(tgnn):
+    """Every step writes to it: a tensor in host memory, of another type or of no element is none that it can write to."""
+    ctx = types.SimpleNamespace(h=None, _clip_norm=None)
+    for bad, word in ((torch.zeros(1), "current GPU"), (torch.zeros(1, dtype=torch.float64), "float32"), (torch.zeros(0), "float32"),
+                      (torch.zeros(2, 2), "float32")):
+        with pytest.raises(ValueError, match=word):
+            tgnn.Context.tgnn_set_grad_clip(ctx, 1.0, bad)
+    assert ctx._clip_norm is None
+    with pytest.raises(tgnn.TgnnError, match="ctx"):       # what is refused here is the context that is not there
+        tgnn.Context.tgnn_set_grad_clip(ctx, 1.0, None)
