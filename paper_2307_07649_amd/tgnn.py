@@ -261,6 +261,7 @@ class Seqs:
                 if t.get_device() != _device_of(t):
                     raise _elsewhere(t, name)
         self.indptr, self.cnt, self.n_rows, self.n_seqs = indptr, cnt, n_rows, n_seqs
+        self.dev = next((t.get_device() for t in (indptr, cnt) if t is not None), None)
         self.c = tgnn_seqs(None if indptr is None else indptr.data_ptr(), None if cnt is None else cnt.data_ptr(), n_rows,
                            _int32(n_seqs, "n_seqs"), _int32(max_len, "max_len"), 1 if newest_first else 0)
 
@@ -268,6 +269,8 @@ class Seqs:
 def _seq_rows(seqs, x):
     if x.dim() == 2 and x.shape[0] != seqs.n_rows:
         raise ValueError(f"x has {x.shape[0]} rows, the sequences {seqs.n_rows}")
+    if seqs.dev is not None and x.get_device() != seqs.dev:
+        raise ValueError(f"x is on {x.device}, the sequences on cuda:{seqs.dev}")
 
 
 def _states(state_in, state_out, state_idx, dev, n, shape, dtype):

@@ -57,3 +57,18 @@ def test_where_the_steps_norm_goes(tgnn):
     assert ctx._clip_norm is None
     with pytest.raises(tgnn.TgnnError, match="ctx"):       # what is refused here is the context that is not there
         tgnn.Context.tgnn_set_grad_clip(ctx, 1.0, None)
+
+
+def test_sequences_of_another_device(tgnn, monkeypatch):
+    """Row ranges that were made on one GPU, and tensors on the one that is current now."""
+    def on(dev, *shape, dtype=torch.float32):
+        t = torch.empty(*shape, dtype=dtype)
+        t.get_device = lambda: dev
+        return t
+    monkeypatch.setattr(tgnn, "_device_of", lambda t: t.get_device())
+    for q in (tgnn.Seqs(4, 2, 4, indptr=on(1, 3, dtype=torch.int64)), tgnn.Seqs(4, 2, 2, cnt=on(1, 2, dtype=torch.int32))):
+        x, A, B = on(0, 4, 8), on(0, 8, 4), on(0, 4, 4)
+        for call in (lambda: tgnn.tgnn_causal_conv_fwd(q, x, A), lambda: tgnn.tgnn_causal_conv_bwd(q, x, x, A),
+                     lambda: tgnn.tgnn_selective_scan_fwd(q, x, x, A, B, B), lambda: tgnn.tgnn_selective_scan_bwd(q, x, x, x, A, B, B)):
+            with pytest.raises(ValueError, match="the sequences on cuda:1"):
+                call()
