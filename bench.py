@@ -276,14 +276,15 @@ def run_config(tgnn, torch, P, args, detail):
         every = max(1, args.event_every)
         ctx.tgnn_profile_enable(roof_mask)
         ctx.tgnn_profile_every(2)             # warm up both launch modes
+        # A full pass of Python's collector over everything that is loaded takes 40 ms, as long as 400 steps of the smallest
+        # workload; where it falls depends on how many objects the imports have made.  It has its pass ahead of the warm-up,
+        # so that the timed steps follow a GPU at work, and none until they are done.
+        gc.collect()
+        gc.disable()
         run_steps(0, args.warmup)
         torch.cuda.synchronize()
         ctx.tgnn_profile_enable(roof_mask)    # drops the warm-up's records
         ctx.tgnn_profile_every(every)
-        # A full pass of Python's collector over everything that is loaded takes 40 ms, as long as 400 steps of the smallest
-        # workload; where it falls depends on how many objects the imports have made.  It has its pass here and none below.
-        gc.collect()
-        gc.disable()
         t0 = time.perf_counter()
         per_step = run_steps(args.warmup, args.warmup + args.steps)
         torch.cuda.synchronize()
