@@ -376,7 +376,7 @@ int32_t tgnn_profile_read(tgnn_ctx* ctx, int32_t stage, int32_t* out_count, doub
  * tgnn_..._workspace_bytes; what it holds before and after does not matter; two calls that may overlap in time need two).
  * Row arrays (x, y, dy, ...) hold float, bfloat16 or float16 values (`dtype`, one type for all row arrays of a call), start at any
  * multiple of the value's size and have their rows `ld_...` values apart (of the convolution's and the scan's: at most 2^27); weights, states and their gradients are float and
- * contiguous.  Arithmetic is in float, sums over many rows in double at the end, and no sum depends on the order in which
+ * contiguous.  Arithmetic is in float, sums over many rows in double at the end (a workgroup's own part of them in float), and no sum depends on the order in which
  * workgroups finish.  What a call writes (states, saved values, the workspace, weights' gradients too) shares memory with nothing else of
  * the call, except where a function says so.  Gradients of weights are added to what is there (accumulate != 0) or written (0); NULL: not wanted. */
 #define TGNN_F32 0
@@ -431,7 +431,8 @@ int32_t tgnn_causal_conv_bwd(const tgnn_seqs* seqs, int32_t dtype, int32_t d, in
 /* Selective state space scan.  Column c has n_state states h, its step size, input and output weights come with the event:
  *   delta = softplus(dt + dt_bias) (dt + dt_bias with softplus = 0),  h[n] = exp(delta A[c, n]) h[n] + delta x B[g, n],
  *   y = (sum over n of C[g, n] h[n] + D[c] x) silu(z)
- * with g = c / (d / n_groups) the column's group.  dt_bias, D NULL: zero; z NULL: no gate. */
+ * with g = c / (d / n_groups) the column's group.  dt_bias, D NULL: zero; z NULL: no gate.  A and the step sizes have to be finite (an infinite one
+ * leaves nothing meaningful in its column, in its events' dB and dC, and in all events of its sequence after, backwards before them); A delta may be positive. */
 typedef struct {
   int32_t dtype, d, n_state, n_groups, softplus, n_states;
   const void *x, *dt, *B, *C, *z;             /* [rows, d] x 2, [rows, n_groups n_state] x 2, [rows, d] */

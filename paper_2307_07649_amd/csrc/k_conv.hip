@@ -8,8 +8,8 @@
 // Bound by memory: a thread has one pack of columns and walks along a segment of a sequence with the last W inputs (and, on the way
 // back, the last W values of g, from which a row of dx is complete) in registers, so that a row is read once; what two
 // neighbouring segments both need (W - 1 rows on either side) is read twice.  Threads of a workgroup that no column is
-// left for take another segment.  29,000 rows of 1,024 columns in bfloat16, four taps: forward 30 us, 4.0 TB/s; backward 63 us, 2.9
-// TB/s, the vector units busy in 56 per cent of the cycles of three wavefronts each; 4,000 single events 18.7 us, 3.5 TB/s.
+// left for take another segment.  29,000 rows of 1,024 columns in bfloat16, four taps: forward 30 us, 4.0 TB/s; backward 62 us, 2.9
+// TB/s, the vector units busy in 53 per cent of the cycles of three wavefronts each; 4,000 single events 18.7 us, 3.5 TB/s.
 #include <algorithm>
 
 #include "seq_device.h"
@@ -366,7 +366,9 @@ template <bool FOUR, class F> static void conv_shape(int dtype, int width, int d
 }
 
 // Rows of a segment, 2^4 to 2^6: as many as leave `waves` wavefronts with four rows each on their way.  What is read
-// twice is 5 per cent with 64 rows and four taps, 20 per cent (out of the L2) with 16.
+// twice is 5 per cent with 64 rows and four taps, 20 per cent (out of the L2) with 16.  (29,000 rows of 1,024 columns in bfloat16, backward, on
+// one set of inputs: 57 us with 3,000, 53 with 1,500, 63 with 6,000; forward, and 7,000 to 120,000 rows of 1,024 to 100 columns,
+// within one per cent of each other with half or twice as many.)
 static int conv_bits(const tgnn_seqs& q, int d, int v, int waves) {
   const int64_t rows = q.indptr == nullptr ? (int64_t)q.n_seqs * q.max_len : q.n_rows, packs = (d + v - 1) / v;
   int bits = 6;

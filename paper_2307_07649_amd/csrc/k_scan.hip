@@ -14,10 +14,12 @@
 //
 // Bound by the vector units: an event costs every state of every column an exponential, two multiplications and two fused ones, forward,
 // and three times as much backward, against 8 to 16 bytes of memory per column.  32 sequences, 29,000 events of 1,024 columns in
-// bfloat16 with 16 states: the segments' own parts 110 us, from segment to segment 19, the outputs 143, the vector units busy in all
-// cycles of the first and last (their memory would take 52).  A sequence of 8,191 events, 512 columns: forward 60 us with the states saved,
-// backward 145, of which 97 in the last walk (busy in 80 per cent of its cycles at the two wavefronts that 212 registers leave a
-// vector unit).  12,000 lists of ten events, 100 columns of float, states in and out: 89 us, 3.8 TB/s, busy in 75 per cent.
+// bfloat16 with 16 states: the segments' own parts 111 us, from segment to segment 22, the outputs 145, the vector units busy in all
+// cycles of the first and last (their memory would take 52); of the 131 instructions that an event costs a wavefront in the outputs 80
+// are the states', the others the step size, the gate, conversions, loads and the way through LDS.  A sequence of 8,191 events, 512 columns
+// in two groups: forward 63 us with the states saved, backward 145, of which 99 in the last walk (busy in 79 per cent of its cycles at the
+// two wavefronts that 212 registers leave a vector unit).  12,000 lists of ten events, 100 columns of float, states in and out: 89 us, 3.8
+// TB/s, busy in 77 per cent.
 //
 // Forward, a lane has a column with all its states in registers: no sum crosses lanes, and B and C of an event are the same for
 // the whole wavefront.  The recurrence along the events is what limits how many wavefronts there are; long sequences are
@@ -269,7 +271,7 @@ __device__ __forceinline__ float times_exp2(float v, float s) {
 // reaches segment k from behind, from zero.  A thread has a column and state of a sequence and asks for eight segments at a time;
 // where there are many of them (RUNS = 8) eight threads cut them into runs: each run's own part and the sum of its
 // deltas, the run's first state from those before it, then the states.  256 segments of 8,192 columns and states: 13 us,
-// one thread for all, one segment after the other, 87; up to 32 segments of 32 sequences of 16,384: 37 us with runs.
+// one thread for all, one segment after the other, 87; up to 32 segments of 32 sequences of 16,384: 37 us with runs, 22 without.
 template <bool BACK, int RUNS>
 __global__ __launch_bounds__(256) void scan_chain_kernel(ScanArgs a) {
   constexpr int COLS = 256 / RUNS;
@@ -356,7 +358,7 @@ __device__ __forceinline__ float rows_sum(float u, float v) {
 }
 
 // Wavefronts and columns of a workgroup.  Wavefronts share what is read of B and C, the sums over columns, and barriers: 1,800 lists of up to ten
-// events, 100 columns, 72 us, one sequence of 8,191 events, 512 columns, 97; with eight 87 and 116, with two 79 and 114, with one 74 and 110.
+// events, 100 columns, 73 us, one sequence of 8,191 events, 512 columns, 99; with eight 87 and 116, with two 79 and 114, with one 74 and 110.
 constexpr int BWD_WAVES = 4, BWD_COLS = 16 * BWD_WAVES;
 constexpr int FINISH_BITS = 3;
 constexpr int SLICE = 16;                                 // states of a column that a workgroup has at most
@@ -376,7 +378,8 @@ __device__ __forceinline__ int event_of_sum(int lane) { return 2 * (lane >> 5) +
 // A workgroup: 16 columns per wavefront of one group, over the pieces worker, worker + workers, ...  With more than 16 states (SLICED)
 // it has 16 of them, n0 .. n0 + 15, and leaves its part of the sums over the states (y0, s1, s2) for scan_finish_kernel.  (With all 64
 // states of a column in four lanes, spilled, one wavefront to a vector unit, forward and backward over 10,000 events of 86 columns and 37
-// states took 419 us, now 235; 1,126 lists of one event, 623 columns, 63 states: 1,311 and 594.)
+// states took 419 us, now 235; 1,126 lists of one event, 623 columns, 63 states: 1,311 and 594.  Narrow models lose by it, since they have
+// wavefronts without a column in every slice: 163 sequences, 40,000 events of 13 columns and 56 states 278 and 366.)
 template <class T, int NP, bool USUAL, bool SLICED>
 __global__ __launch_bounds__(64 * BWD_WAVES, 2) void scan_bwd_kernel(ScanArgs a) {
   constexpr int WAVES = BWD_WAVES, THREADS = 64 * WAVES, N4 = 4 * NP, STAGE = CHUNK * N4 / THREADS > 0 ? CHUNK * N4 / THREADS : 1;
