@@ -716,8 +716,10 @@ class Context:
                                        eps))
 
     def tgnn_set_grad_clip(self, max_norm, out_norm=None):
-        """max_norm of the in-step update's gradients, 0: none; out_norm: float32 device tensor [1], every step's norm."""
-        norm = None if out_norm is None else _floats(out_norm, "out_norm", _device_of(out_norm), (1,))
+        """max_norm of the in-step update's gradients, 0: none; out_norm: float32 device tensor, whose first value is every step's norm."""
+        if out_norm is not None and out_norm.numel() == 0:
+            raise ValueError("out_norm: a float32 tensor of one value is needed")
+        norm = None if out_norm is None else _floats(out_norm, "out_norm", _device_of(out_norm), out_norm.shape)
         _check(_lib.tgnn_set_grad_clip(self.h, max_norm, norm))
         self._clip_norm = out_norm      # keeps it alive
 
